@@ -190,6 +190,7 @@ def prepare(case, seed):
             pages = case["pages"]
         shape = (pages, kh, page)
         s["codes"] = [_nibbles(gen, shape + (d,)) for _ in range(2)]
+        s["codes"][1] = s["codes"][1].transpose(2, 3).contiguous()           # values: a channel pair's tokens side by side
         s["steps"] = [torch.randint(40, 100, shape + (_groups(d),), generator=gen, **dev).to(torch.uint8) for _ in range(2)]
         order = torch.randperm(pages, generator=gen, **dev).to(torch.int32)
         if k == "store":
@@ -315,6 +316,7 @@ def _plain_store(s):
         a = x.abs().amax(-1, keepdim=True)
         c = torch.div(14 * x.abs() + a, (2 * a).clamp(min=1), rounding_mode="floor") * x.sign()
         c = c.view(-1, kh, _groups(d) * GROUP)[..., :d] & 15
+        codes = codes if rows is s["k"] else codes.transpose(2, 3)
         codes[at, :, pos] = (c[..., 0::2] | (c[..., 1::2] << 4)).to(torch.uint8)
         steps[at, :, pos] = a[..., 0].to(torch.uint8)
     return s["codes"] + s["steps"]
@@ -339,7 +341,7 @@ def _plain_decode(s):
     keep = (torch.arange(m, device="cuda") <= last[:, :, None])[:, None, None]
     w = _weights(x, keep, c)
     total = w.sum(-1, dtype=torch.int64)[..., None]
-    v, va = read(s["codes"][1], s["steps"][1])
+    v, va = read(s["codes"][1].transpose(2, 3), s["steps"][1])
     u = _rshr(w.view(n, kh, 1, e, m) * va.permute(0, 1, 3, 2)[:, :, :, None], 7).double()
     v = torch.nn.functional.pad(v, (0, -d % GROUP)).view(n, kh, m, g, GROUP).permute(0, 1, 3, 2, 4).double().contiguous()
     acc = torch.matmul(u, v).to(torch.int64)                                # [n, kh, g, e, GROUP]
@@ -507,7 +509,8 @@ def exact(case, seed):
         live = torch.tensor([i for i, v in enumerate(slots) if v >= 0], device="cuda", dtype=torch.int64)
         to = torch.tensor([v for v in slots if v >= 0], device="cuda", dtype=torch.int64)
         for rows, codes, steps in zip((s["k"], s["v"]), s["codes"], s["steps"]):
-            flat_c = codes.transpose(1, 2).reshape(-1, kh, d // 2).clone()
+            by_token = codes if rows is s["k"] else codes.transpose(2, 3)
+            flat_c = by_token.transpose(1, 2).reshape(-1, kh, d // 2).clone()
             flat_s = steps.transpose(1, 2).reshape(-1, kh, _groups(d)).clone()
             for g in range(_groups(d)):
                 x = rows[live][:, :, g * GROUP:min(d, (g + 1) * GROUP)].to(torch.int64)
@@ -517,7 +520,7 @@ def exact(case, seed):
                 at = g * GROUP // 2
                 flat_c[to, :, at:at + x.shape[-1] // 2] = (code[..., 0::2] + 16 * code[..., 1::2]).to(torch.uint8)
                 flat_s[to, :, g] = a[..., 0].to(torch.uint8)
-            codes.copy_(flat_c.view(-1, page, kh, d // 2).transpose(1, 2))
+            by_token.copy_(flat_c.view(-1, page, kh, d // 2).transpose(1, 2))
             steps.copy_(flat_s.view(-1, page, kh, _groups(d)).transpose(1, 2))
         return s["codes"] + s["steps"]
     if k == "decode":
@@ -528,7 +531,7 @@ def exact(case, seed):
             seen = n - t + 1 + torch.arange(t, device="cuda")
             for b in range(kh):
                 (kc, ka), (vc, va) = ((_unpacked(x[at, b].reshape(-1, d // 2)[:n]), y[at, b].reshape(-1, _groups(d))[:n].to(torch.int64))
-                                      for x, y in zip(s["codes"], s["steps"]))
+                                      for x, y in zip((s["codes"][0], s["codes"][1].transpose(2, 3)), s["steps"]))
                 key = kc * torch.cat([ka[:, g:g + 1].expand(-1, min(GROUP, d - g * GROUP)) for g in range(_groups(d))], 1)
                 for head in range(b * (h // kh), (b + 1) * (h // kh)):
                     w = _exact_rows(s["q"][i * t:(i + 1) * t, head], key, seen, c)
