@@ -16,7 +16,8 @@
  *     as their output buffers do not.
  *   - Arithmetic conventions: x >> k on a negative integer is floor(x / 2^k);
  *     rshr_round(v, s) = (v + 2^(s-1)) >> s for s >= 1 and v for s == 0 (ties go up).
- *   - The kernels contain integer instructions only (no floating point, no matrix cores).
+ *   - The kernels contain integer instructions only: no floating point; matrix cores (their integer forms) in
+ *     the two attentions only.
  */
 #ifndef IPTQ_H
 #define IPTQ_H
@@ -34,6 +35,7 @@ extern "C" {
 #define IPTQ_ERR_RANGE (-4) /* parameters are valid one by one but could overflow the fixed-width path */
 #define IPTQ_ERR_HIP (-5)   /* the HIP runtime refused the launch */
 #define IPTQ_ERR_ALIGN (-6) /* a pointer is not aligned to its element type */
+#define IPTQ_ERR_WORKSPACE (-7) /* the workspace is smaller than the call needs */
 
 #define IPTQ_COLS_MAX 65536
 
@@ -317,6 +319,147 @@ int iptq_softmax_prepare(double s_delta, int32_t cols, int32_t variant, int32_t 
  * post = dyadic(s_in * a * S_e^p * 2^k / 2 / s_out), zero-point zp_out, int8 clip. */
 int iptq_gelu_prepare(double s_in, double s_out, int32_t zp_in, int32_t zp_out, int32_t variant,
                       int32_t max_abs_q, iptq_gelu_params_t *out);
+
+/*
+ * Operators of a transformer block beside its softmax and GELU, in the same integer arithmetic: attention over
+ * packed prompts, a 4-bit key/value cache and the attention of single tokens over it, the root-mean-square norm
+ * with the residual's addition, requantization by row scales.  The products inside the attention run on
+ * the matrix cores' integer forms; there is no floating point.  The general rules above hold.
+ */
+
+/*
+ * Attention weights and output.  Of one query q with keys k_j and values v_j (int8 each):
+ *   1. x_j = q . k_j (int32), x_j = rshr_round(x_j, score_shift)
+ *   2. w_j = Qexp_j of the softmax's steps 1-5 with this variant, i0 and n_shift: at most i0 << n_shift
+ *   3. f = floor(2^54 / sum_j w_j) (0 for a query that sees no key),
+ *      o_d = (f * sum_j w_j v_jd) >> 46: the mean of the values with eight fractional bits.  The division of
+ *      Eq. 15 comes after the product here, once per output: no probability is cut to eight bits,
+ *      which over long rows would leave nothing of most of them.
+ *   4. out_d = clamp(rshr_round(o_d * post.m, post.s) + post.zp, post.qmin, post.qmax), int8
+ * Domain: variant in {0,1,2}; 16 <= i0 <= 1024; n_shift >= 0, (i0 << n_shift) <= IPTQ_WEIGHT_MAX (else
+ * IPTQ_ERR_RANGE); 0 <= score_shift <= IPTQ_SCORE_SHIFT_MAX (IPTQ_CACHE_SCORE_SHIFT_MAX over the cache); causal in {0,1}.
+ */
+#define IPTQ_WEIGHT_MAX 32639
+#define IPTQ_SCORE_SHIFT_MAX 16
+#define IPTQ_CACHE_SCORE_SHIFT_MAX 20
+typedef struct {
+    int32_t variant;     /* IPTQ_SOFTMAX_* */
+    int32_t i0;          /* floor(1 / scale of the shifted scores) */
+    int32_t n_shift;
+    int32_t score_shift;
+    int32_t causal;
+    iptq_dyadic_t post;  /* int8 output */
+} iptq_attention_params_t;
+
+/*
+ * Attention over packed sequences.  d_q: q_tokens rows of heads * head_dim int8, q_stride bytes apart; d_k, d_v:
+ * k_tokens rows of kv_heads * head_dim, k_stride and v_stride apart (so all three may lie in the rows of one
+ * product's output); d_out as d_q with out_stride.  No alignment is asked.  heads is a multiple of kv_heads, head h
+ * reads the keys of head h div (heads / kv_heads).  head_dim: 32, 64, 96 or 128.
+ * Sequence i has queries d_q_offsets[i] .. d_q_offsets[i + 1] - 1 and keys d_k_offsets[i] .. d_k_offsets[i + 1] - 1
+ * (n_seq + 1 int32 each, device, not decreasing); both NULL: equal lengths, q_tokens / n_seq and k_tokens / n_seq (no
+ * remainder, else IPTQ_ERR_SHAPE).  causal: the last query of a sequence sees all its keys, the one before it all but the last,
+ * and so on (a sequence with more queries than keys has queries that see none: their output is the step 4 of 0).
+ * max_q: the longest sequence's number of queries; those beyond it, and rows of d_out that belong to no sequence, are left
+ * as they were.  Offsets are read on the device and clamped to [0, tokens]; a sequence of more than
+ * IPTQ_KEYS_MAX keys is not served, its rows are left as they were.  n_seq, max_q or q_tokens 0: a no-op.
+ * d_out must not overlap an input.  max_q (rounded up to 32) / 32 * n_seq * heads < 2^31.
+ */
+#define IPTQ_KEYS_MAX 65536
+int iptq_attention_i8(const int8_t *d_q, int64_t q_stride, const int8_t *d_k, int64_t k_stride, const int8_t *d_v, int64_t v_stride,
+                      const int32_t *d_q_offsets, const int32_t *d_k_offsets, int32_t n_seq, int32_t max_q, int64_t q_tokens,
+                      int64_t k_tokens, int32_t heads, int32_t kv_heads, int32_t head_dim, int8_t *d_out, int64_t out_stride,
+                      const iptq_attention_params_t *p, void *stream);
+
+/*
+ * A cache of keys and values in pages, four bits per value.  64 channels (the last group of a row may have 32) of one
+ * token and kv head share a step a = max |x|; the code of x is c = sign(x) floor((14 |x| + a) / (2 a)) in
+ * [-7, 7] (0 where a is 0), which stands for c a / 7.
+ * Layout (device, caller-owned, 16-byte aligned): d_k_codes [n_pages, kv_heads, page_tokens, head_dim / 2],
+ * d_v_codes [n_pages, kv_heads, head_dim / 2, page_tokens] (the products want the keys' channels and the values' tokens
+ * side by side), byte b of either holds channel 2 b in its low half and 2 b + 1 in its high half, two's complement; d_k_steps,
+ * d_v_steps [n_pages, kv_heads, page_tokens, ceil(head_dim / 64)], values up to 128.
+ * page_tokens: a power of two from 16 to 4096; head_dim: 32, 64, 96 or 128; n_pages * page_tokens < 2^31.
+ */
+typedef struct {
+    uint8_t *d_k_codes, *d_k_steps, *d_v_codes, *d_v_steps;
+    int32_t n_pages, page_tokens, kv_heads, head_dim;
+} iptq_cache_i4_t;
+
+/*
+ * Stores `tokens` rows of keys and values (int8, as in iptq_attention_i8) into the cache: row i goes to
+ * slot d_slots[i] = page * page_tokens + position (int32, device).  A slot outside [0, n_pages * page_tokens) is skipped
+ * (padding: -1).  No two rows of a call may name the same slot (what that slot then holds is not
+ * specified; nothing else is touched).
+ */
+int iptq_cache_store_i4(const iptq_cache_i4_t *cache /*host*/, const int8_t *d_k, int64_t k_stride, const int8_t *d_v, int64_t v_stride,
+                        const int32_t *d_slots, int64_t tokens, void *stream);
+
+/*
+ * Attention of the last q_tokens tokens of each of n_seq sequences over the cache: d_q and d_out hold rows
+ * [n_seq, q_tokens] of heads * head_dim int8.  Sequence i has d_lengths[i] tokens in the cache (int32, device; the new
+ * ones among them, stored before), token t in page d_pages[i * max_pages + t div page_tokens] (int32, device).  causal: of
+ * the q_tokens the last sees all, the one before it all but the last token, and so on; else each sees all.
+ * The steps of iptq_attention_params_t, in integers throughout:
+ *   x_j = sum over groups of a_jg (q_g . c_jg): seven times the product of the values the codes stand for (the
+ *   factor belongs to the score's scale), then steps 1 and 2;
+ *   u_jg = rshr_round(w_j a'_jg, 7) with the step a' of the value's group: a rounding to the 15 bits of a weight, so that both halves
+ *   of it fit a signed byte; o_d = (f * sum_j u_j c'_jd) >> 39, seven times the mean with eight fractional bits; step 4.
+ * Lengths are clamped to [0, max_pages * page_tokens]; tokens in a page outside [0, n_pages) count as masked and
+ * are not read.  A query that sees no key gives the step 4 of 0.  1 <= q_tokens <= IPTQ_CACHE_QUERIES_MAX,
+ * max_pages * page_tokens <= IPTQ_CACHE_KEYS_MAX, n_seq * q_tokens * heads < 2^24.
+ * d_work: iptq_attention_cache_i4_workspace bytes (16-byte aligned; IPTQ_ERR_WORKSPACE if there are fewer; it may be
+ * NULL where that is 0).  Its contents need no preparation and mean nothing afterwards; calls that may run at the same time need
+ * one each.  d_out and d_work must not overlap an input or each other.
+ */
+#define IPTQ_CACHE_QUERIES_MAX 64
+#define IPTQ_CACHE_KEYS_MAX 131072
+int iptq_attention_cache_i4_workspace(const iptq_cache_i4_t *cache /*host*/, int32_t n_seq, int32_t q_tokens, int32_t heads, int32_t max_pages,
+                                      int64_t *bytes /*host*/);
+int iptq_attention_cache_i4(const int8_t *d_q, int64_t q_stride, const iptq_cache_i4_t *cache /*host*/, const int32_t *d_pages, int32_t max_pages,
+                            const int32_t *d_lengths, int32_t n_seq, int32_t q_tokens, int32_t heads, int8_t *d_out, int64_t out_stride,
+                            void *d_work, int64_t work_bytes, const iptq_attention_params_t *p, void *stream);
+
+/*
+ * Root-mean-square norm of every row of a row-major [rows, cols] tensor, with the addition to the residual stream in front
+ * and 8-bit codes behind.  With L = 2^23 - 1:
+ *   1. r_i = clamp(residual_i + rshr_round(x_i * in_m, in_s), -L, L): the updated stream (d_x or d_residual may be
+ *      NULL: that term is 0)
+ *   2. S = min(sum_i r_i^2 + cols * eps, 2^62 - 1); t = floor((62 - bitlen(S)) / 2);
+ *      R = floor(sqrt(S 2^(2t))); F = (floor(sqrt(cols 2^32)) * floor(2^61 / R)) >> 24 (0 if S is 0)
+ *   3. z_i = rshr_round(r_i * F, 41 - t): r_i over the root of the mean square, twelve fractional bits
+ *   4. y_i = rshr_round(z_i * gain_i, 6)                                    (|y_i| <= 2^29)
+ *   5. d_row_scales NULL: out_i = clamp(rshr_round(y_i * post.m, post.s) + post.zp, post.qmin, post.qmax);
+ *      else A = max_i |y_i| goes to d_row_scales[row], out_i = rshr_round(y_i * floor(127 * 2^40 / A), 40) (0 if A is 0), which
+ *      stands for out_i * A / 127, and post plays no part
+ * d_x, d_residual: rows * cols int32 (device); d_gain: cols int16; d_out: rows * cols int8; d_row_scales: NULL or rows int32;
+ * d_residual_out: NULL or rows * cols int32 (r; may be d_residual itself, in place).  No other overlap of an output.
+ * |in_m| < 2^15; 0 <= in_s <= 62; 0 <= eps <= 2^46 (in units of the stream's squares); 1 <= cols <= IPTQ_NORM_COLS_MAX.
+ */
+#define IPTQ_NORM_COLS_MAX 32768
+typedef struct {
+    int32_t in_m, in_s;
+    int64_t eps;
+    iptq_dyadic_t post; /* int8 output */
+} iptq_rmsnorm_params_t;
+int iptq_rmsnorm_i32(const int32_t *d_x, const int32_t *d_residual, const int16_t *d_gain, int32_t *d_residual_out, int8_t *d_out,
+                     int32_t *d_row_scales, int64_t rows, int32_t cols, const iptq_rmsnorm_params_t *p, void *stream);
+
+/*
+ * Requantization of a row-major [rows, cols] int32 tensor whose rows have scales of their own (the product of codes that
+ * iptq_rmsnorm_i32 made with row scales): v = sat32(rshr_round(x * d_row_scales[row], row_shift)), then the step p of v.
+ * d_row_scales: rows int32 (device); output as in iptq_requant.  0 <= row_shift <= 62; 1 <= cols <= IPTQ_ROW_COLS_MAX.
+ */
+#define IPTQ_ROW_COLS_MAX 1048576
+int iptq_requant_rows(const int32_t *d_in, const int32_t *d_row_scales, int32_t row_shift, void *d_out, int64_t rows, int32_t cols,
+                      int32_t out_is_signed, const iptq_dyadic_t *p, void *stream);
+
+/* Host-only: constants of an attention from real scales.  s_score: scale of the int32 products q . k (softmax's 1 / sqrt(head_dim)
+ * in it); s_v, s_out: scales of the values and of the output; of_cache: 1 for iptq_attention_cache_i4 (scores and values
+ * count sevenths there).  score_shift is the smallest that brings 1 / scale below 1025, n_shift the largest.
+ * IPTQ_ERR_RANGE where the scale is coarser than 1/16 or too fine. */
+int iptq_attention_prepare(double s_score, double s_v, double s_out, int32_t zp_out, int32_t variant, int32_t causal, int32_t of_cache,
+                           iptq_attention_params_t *out);
 
 /*
  * Host-only: the Unified Metric that picks the approximation function of each activation layer

@@ -27,6 +27,10 @@ SOURCES = ["softmax_long_p13_16.hip", "softmax_long_p9_12.hip", "softmax_long_p7
            "softmax_rowsdyn_k16.hip", "softmax_kernels.hip", "elementwise_kernels.hip",
            "softmax_rowsdyn.hip", "softmax_wide.hip", "softmax_wgrow.hip", "softmax_long.hip", "api.hip", "debug_hooks.hip",
            "plan.cpp", "metric.cpp"]
+# the block operators (attention, cache, norm), in csrc/block
+BLOCK = os.path.join(CSRC, "block")
+BLOCK_SOURCES = ["attention_i8_128.hip", "attention_i8_96.hip", "attention_i8_64.hip", "attention_i8_32.hip", "cache_i4.hip",
+                 "attention_i8.hip", "norm.hip", "plan_block.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",
          "-Wno-unused-parameter",
          # packed-FP32 instructions stay off: the kernels are integer-only anyway
@@ -36,14 +40,13 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextr
 def build(extra_flags=(), verbose: bool = False, lib: str = LIB, obj_dir: str = OBJ) -> str:
     os.makedirs(obj_dir, exist_ok=True)
 
-    def one(src):
-        obj = os.path.join(obj_dir, os.path.splitext(src)[0] + ".o")
-        subprocess.check_call(["hipcc", "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj] + FLAGS
-                              + list(extra_flags))
+    def one(path):
+        obj = os.path.join(obj_dir, os.path.splitext(os.path.basename(path))[0] + ".o")
+        subprocess.check_call(["hipcc", "-x", "hip", "-c", path, "-o", obj] + FLAGS + list(extra_flags))
         return obj
 
     with ThreadPoolExecutor(max_workers=8) as ex:
-        objs = list(ex.map(one, SOURCES))
+        objs = list(ex.map(one, [os.path.join(CSRC, s) for s in SOURCES] + [os.path.join(BLOCK, s) for s in BLOCK_SOURCES]))
     tmp = lib + ".tmp%d" % os.getpid()
     subprocess.check_call(["hipcc", "-shared", "-fPIC", "--offload-arch=gfx950", "-o", tmp] + objs)
     os.replace(tmp, lib)

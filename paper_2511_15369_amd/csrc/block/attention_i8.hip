@@ -1,0 +1,30 @@
+// Attention over packed prompts: the launch.
+#include "attention_i8.h"
+
+namespace iptq {
+
+hipError_t attention_i8_dispatch(const AttentionCall &c, hipStream_t stream)
+{
+    AttentionArgs a;
+    a.q = c.q; a.k = c.k; a.v = c.v; a.out = c.out;
+    a.q_stride = c.q_stride; a.k_stride = c.k_stride; a.v_stride = c.v_stride; a.out_stride = c.out_stride;
+    a.q_offsets = c.q_offsets; a.k_offsets = c.k_offsets;
+    a.q_tokens = (int32_t)c.q_tokens; a.k_tokens = (int32_t)c.k_tokens;
+    a.q_len = (int32_t)(c.q_tokens / c.n_seq); a.k_len = (int32_t)(c.k_tokens / c.n_seq);
+    a.max_q = c.max_q;
+    a.kv_heads = c.kv_heads; a.group = c.heads / c.kv_heads;
+    a.by_kv_heads = div_of((uint32_t)c.kv_heads);
+    a.by_group = div_of((uint32_t)a.group);
+    a.by_seq = div_of((uint32_t)c.n_seq);
+    a.tiles = ((uint32_t)c.max_q + kQueries - 1) / kQueries;
+    a.P = c.P;
+    const uint32_t grid = a.tiles * (uint32_t)c.n_seq * (uint32_t)c.heads;      // below 2^31: checked
+    switch (c.dim) {
+    case 32: return attention_i8_launch_32(a, grid, stream);
+    case 64: return attention_i8_launch_64(a, grid, stream);
+    case 96: return attention_i8_launch_96(a, grid, stream);
+    default: return attention_i8_launch_128(a, grid, stream);
+    }
+}
+
+}  // namespace iptq

@@ -1,0 +1,197 @@
+// Operators of a transformer block beside its softmax and GELU: launch records, host entry points of the
+// kernel files and the integer helpers they share.  Like the kernels one folder up these hold integer
+// instructions only; the products of queries with keys and of weights with values run on the matrix cores'
+// integer forms (v_mfma_i32).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../device_common.h"
+#include "../plan.h"
+
+namespace iptq {
+
+typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kGroup = 64;            // channels that share one step of the 4-bit cache
+constexpr int kGroupsMost = 2;        // head dimensions go up to 128
+
+// Unsigned division by a run-time constant (the compiler's own goes through floating point).
+struct DivDev {
+    uint32_t d, magic;
+    int32_t sh;
+};
+inline DivDev div_of(uint32_t d)      // 1 <= d, dividends below 2^31
+{
+    DivDev v = {d, 0, 0};
+    if (d > 1) make_magic_u32(d, 31, &v.magic, &v.sh);
+    return v;
+}
+IPTQ_HD uint32_t div_by(uint32_t n, const DivDev &D) { return D.d == 1 ? n : mulhi_u32(n, D.magic) >> D.sh; }
+
+// Constants of an attention's exponentials and of its output step.
+struct AttentionDev {
+    int32_t variant, i0, i0n, n_shift;
+    int32_t d_clamp;                  // deltas below -D have weight 0
+    int32_t div8;                     // byte divider by i0 (SoftmaxDev::div8)
+    uint32_t d2_magic;                // second degree: division by 2 i0
+    int32_t d2_sh;
+    int32_t shift;                    // scores are brought to i0's scale by a rounding shift
+    int32_t causal;
+    DyadicDev post;
+};
+
+struct AttentionCall {
+    const int8_t *q, *k, *v;
+    int8_t *out;
+    int64_t q_stride, k_stride, v_stride, out_stride;     // bytes between two tokens
+    const int32_t *q_offsets, *k_offsets;                 // [n_seq + 1] on the device, or nullptr: equal lengths
+    int64_t q_tokens, k_tokens;
+    int32_t n_seq, max_q, heads, kv_heads, dim;
+    AttentionDev P;
+};
+
+struct CacheDev {
+    uint8_t *k_codes, *k_steps, *v_codes, *v_steps;
+    int32_t n_pages, page_tokens, page_log, kv_heads, dim;
+};
+
+struct CacheAttentionCall {
+    const int8_t *q;
+    int8_t *out;
+    int64_t q_stride, out_stride;
+    const int32_t *pages, *lengths;
+    int32_t n_seq, max_pages, q_tokens, heads;
+    void *work;
+    CacheDev C;
+    AttentionDev P;
+};
+
+struct CacheStoreCall {
+    const int8_t *k, *v;
+    int64_t k_stride, v_stride;
+    const int32_t *slots;
+    int64_t tokens;
+    CacheDev C;
+};
+
+struct RmsnormCall {
+    const int32_t *x, *residual;
+    int32_t *residual_out;
+    const int16_t *gain;
+    int8_t *out;
+    int32_t *row_scales;
+    int64_t rows;
+    int32_t cols;
+    int32_t in_m, in_s;
+    int64_t eps_sum;                  // cols * eps
+    uint32_t root_cols;               // floor(sqrt(cols) 2^16)
+    DyadicDev post;
+};
+
+hipError_t attention_i8_dispatch(const AttentionCall &c, hipStream_t stream);
+hipError_t cache_store_i4_dispatch(const CacheStoreCall &c, hipStream_t stream);
+int64_t attention_cache_i4_workspace_bytes(const CacheAttentionCall &c);
+hipError_t attention_cache_i4_dispatch(const CacheAttentionCall &c, hipStream_t stream);
+hipError_t rmsnorm_i32_dispatch(const RmsnormCall &c, hipStream_t stream);
+hipError_t requant_rows_dispatch(const int32_t *in, const int32_t *row_scales, int32_t row_shift, void *out, int64_t rows,
+                                 int32_t cols, const DyadicDev &P, hipStream_t stream);
+
+// floor(num / den), num < 2^63, den >= 1 (0 for den == 0): quotients by a 32-bit reciprocal of den that is
+// never too large (Newton's iteration, as floor_pow2_div), the remainder divided again until it is below
+// den.  A step leaves less than 2^-27 of the remainder, so three or four do.
+IPTQ_HD uint64_t floor_div_u64(uint64_t num, uint32_t den)
+{
+    if (den == 0) return 0;
+    const int k = clz_u32(den);
+    const uint32_t y = den << k;
+    uint32_t r = (3031741620u - mulhi_u32(y, 2021161080u)) << 1;
+    for (int it = 0; it < 3; ++it) r = mulhi_u32(r, 0u - mulhi_u32(y, r)) << 1;
+    r -= 4;                                               // within 2 of 2^63 / y for every y: never above it from here on
+    uint64_t q = 0;
+    while (num >= den) {
+        const uint64_t p = (num >> 32) * r + (((num & 0xffffffffu) * r) >> 32);     // num r / 2^32
+        uint64_t e = p >> (31 - k);
+        e = e == 0 ? 1 : e;
+        q += e;
+        num -= e * den;
+    }
+    return q;
+}
+
+// floor(sqrt(v)) for 2^60 <= v < 2^62, one bit of the root after another from the top.
+IPTQ_HD uint32_t root_u62(uint64_t v)
+{
+    uint32_t root = 1u << 30;
+    for (uint32_t bit = 1u << 29; bit != 0; bit >>= 1) {
+        const uint32_t t = root | bit;
+        root = (uint64_t)t * t <= v ? t : root;
+    }
+    return root;
+}
+
+// ---- what the device reads of tables and offsets, kept inside the tensors -----------------------------------
+// Tokens [from, from + n) of a sequence with offsets a and b, inside [0, tokens).
+IPTQ_HD void clamped_range(int32_t a, int32_t b, int32_t tokens, int32_t *from, int32_t *n)
+{
+    *from = a < 0 ? 0 : a > tokens ? tokens : a;
+    *n = (b < *from ? *from : b > tokens ? tokens : b) - *from;
+}
+
+// The page of a sequence's key, or -1 where the sequence or the cache has none.
+IPTQ_HD int32_t page_of_key(const int32_t *table, int page_log, int32_t n_pages, int32_t key, int32_t length)
+{
+    if (key >= length) return -1;
+    const int32_t page = table[key >> page_log];
+    return page >= 0 && page < n_pages ? page : -1;
+}
+
+// ---- weights ------------------------------------------------------------------------------------
+// The bit-shifting exponentials of two scores side by side in 16-bit halves: `d` is the stabilised score of
+// either, clamped at -D, the result (base << N) >> q below 2^15 - 128 (Eq. 7-10, 13-14; the second degree).
+template <int VARIANT>
+IPTQ_DEV uint32_t weights_of_pair(i16x2 d, const AttentionDev &P)
+{
+    const i16x2 m = (d + (d >> (short)1)) - (d >> (short)4);           // Qp of Eq. 7, in (-2^15, 0]
+    const uint32_t mw = __builtin_bit_cast(uint32_t, m);
+    // Eq. 8: (-m) div i0 is the top byte of (-m) ceil(2^24 / i0), both factors negated
+    const uint32_t a = (uint32_t)__mul24((int32_t)(int16_t)mw, P.div8);
+    const uint32_t b = (uint32_t)__mul24((int32_t)mw >> 16, P.div8);
+    const u16x2_t q = __builtin_bit_cast(u16x2_t, (uint32_t)__builtin_amdgcn_perm(b, a, 0x0c070c03u));
+    const i16x2 nr = (i16x2)(q * (unsigned short)P.i0 + (u16x2_t)m);   // -r in (-i0, 0]
+    i16x2 fr = nr >> (short)1;                                         // Eq. 10
+    if (VARIANT >= 1) fr = fr + (nr >> (short)3) + (nr >> (short)4);   // Eq. 13
+    if (VARIANT == 2) {                                                // Eq. 11, second degree
+        const int32_t y0 = fr[0], y1 = fr[1];
+        i16x2 t;
+        t[0] = (short)(mulhi_u32((uint32_t)__mul24(y0, y0), P.d2_magic) >> P.d2_sh);
+        t[1] = (short)(mulhi_u32((uint32_t)__mul24(y1, y1), P.d2_magic) >> P.d2_sh);
+        fr = fr + t;
+    }
+    const u16x2_t base = (u16x2_t)fr * (unsigned short)(1u << P.n_shift) + (unsigned short)P.i0n;
+    return __builtin_bit_cast(uint32_t, (u16x2_t)(base >> q));         // q <= 15
+}
+
+// Weights as the two 8-bit factors of a signed matrix product: w = 256 hi + lo with lo in [-128, 127], so
+// hi = (w + 128) >> 8 is at most 127 for w <= 32639.  Two pairs of weights -> four bytes of each.
+IPTQ_DEV void split_weights(uint32_t w01, uint32_t w23, uint32_t *hi, uint32_t *lo)
+{
+    const u16x2_t half = {128, 128};
+    const uint32_t a = __builtin_bit_cast(uint32_t, (u16x2_t)(__builtin_bit_cast(u16x2_t, w01) + half));
+    const uint32_t b = __builtin_bit_cast(uint32_t, (u16x2_t)(__builtin_bit_cast(u16x2_t, w23) + half));
+    *hi = __builtin_amdgcn_perm(b, a, 0x07050301u);
+    *lo = __builtin_amdgcn_perm(w23, w01, 0x06040200u);
+}
+
+// One output byte: floor(2^54 / total) times the sum of weighted values, shifted, requantized.
+IPTQ_DEV int32_t mean_byte(uint64_t f, int64_t acc, int shift, const DyadicDev &post)
+{
+    const int64_t o = (int64_t)(f * (uint64_t)acc) >> shift;
+    return requant_dev<false>((int32_t)o, post.m, post.s, post.zp, post.qmin, post.qmax);
+}
+
+}  // namespace iptq

@@ -241,7 +241,7 @@ int plan_gelu(const iptq_gelu_params_t *p, int is_i8_entry, GeluDev *out)
 
 // ------------------------------------------------------------------ C ABI: host helpers
 
-extern "C" int iptq_version(void) { return 200; }   // 0.2.0: window masks, second-degree exponential, Unified Metric
+extern "C" int iptq_version(void) { return 300; }   // 0.3.0: attention, 4-bit cache, root-mean-square norm, row scales
 
 extern "C" const char *iptq_strerror(int code)
 {
@@ -253,6 +253,7 @@ extern "C" const char *iptq_strerror(int code)
     case IPTQ_ERR_RANGE: return "parameters could overflow the fixed-width integer path";
     case IPTQ_ERR_HIP: return "the HIP runtime refused the launch";
     case IPTQ_ERR_ALIGN: return "a pointer is not aligned to its element type";
+    case IPTQ_ERR_WORKSPACE: return "the workspace is smaller than the call needs";
     default: return "unknown iptq error code";
     }
 }
