@@ -29,7 +29,8 @@ SOURCES = ["softmax_long_p13_16.hip", "softmax_long_p9_12.hip", "softmax_long_p7
            "plan.cpp", "metric.cpp"]
 # the block operators (attention, cache, norm), in csrc/block
 BLOCK = os.path.join(CSRC, "block")
-BLOCK_SOURCES = ["attention_i8_128.hip", "attention_i8_96.hip", "attention_i8_64.hip", "attention_i8_32.hip", "cache_i4.hip",
+BLOCK_SOURCES = ["attention_i8_128.hip", "attention_i8_96.hip", "attention_i8_64.hip", "attention_i8_32.hip", "attention_cache_i4_128.hip",
+                 "attention_cache_i4_96.hip", "attention_cache_i4_64.hip", "attention_cache_i4_32.hip", "attention_cache_i4.hip", "cache_i4.hip",
                  "attention_i8.hip", "norm.hip", "plan_block.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",
          "-Wno-unused-parameter",

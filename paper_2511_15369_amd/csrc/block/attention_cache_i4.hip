@@ -1,0 +1,132 @@
+// Attention over the 4-bit cache: how the keys are divided, the launches, and the last one, which adds up the splits.
+#include "attention_cache_i4.h"
+
+namespace iptq {
+
+// One column of one sequence per workgroup: 16 threads of eight channels each, 16 of these over the splits.
+__global__ __launch_bounds__(256) void attention_cache_i4_join_kernel(const CacheAttentionArgs A)
+{
+    __shared__ int64_t parts[4][16][8];
+    __shared__ uint32_t totals[4];
+    const uint32_t pair = div_by(blockIdx.x, A.by_chunks), column = blockIdx.x - pair * A.by_chunks.d;     // by_chunks: columns here
+    const uint32_t seq = div_by(pair, A.by_kv_heads), kvh = pair - seq * A.by_kv_heads.d;
+    const int dim = A.C.dim, unit = threadIdx.x & 15, part = threadIdx.x >> 4, wave = threadIdx.x >> 6;
+    const int32_t length = min(max(A.lengths[seq], 0), A.max_pages << A.C.page_log);
+    const int32_t live = (int32_t)div_by((uint32_t)(length + A.split_keys - 1), A.by_splits);              // by_splits: keys here
+    int64_t v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    uint32_t s = 0;
+    if (8 * unit < dim)
+        for (int32_t i = part; i < live; i += 16) {
+            const int64_t at = ((int64_t)pair * A.splits + i) * A.columns + column;
+            const i32x4 *o = reinterpret_cast<const i32x4 *>(A.partial + at * dim + 8 * unit);
+            const i32x4 a = o[0], b = o[1];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { v[j] += a[j]; v[4 + j] += b[j]; }
+            s += A.sums[at];
+        }
+#pragma unroll
+    for (int m = 16; m < 64; m <<= 1) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += __shfl_xor((long long)v[j], m);
+        s += (uint32_t)__shfl_xor((int32_t)s, m);
+    }
+    if ((threadIdx.x & 63) < 16) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) parts[wave][unit][j] = v[j];
+        if (unit == 0) totals[wave] = s;
+    }
+    __syncthreads();
+    if (threadIdx.x >= 16 || 8 * unit >= dim) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = parts[0][unit][j] + parts[1][unit][j] + parts[2][unit][j] + parts[3][unit][j];
+    const uint64_t f = floor_div_u64((uint64_t)1 << 54, totals[0] + totals[1] + totals[2] + totals[3]);
+    const uint32_t token = div_by(column, A.by_group), head = kvh * (uint32_t)A.group + (column - token * (uint32_t)A.group);
+    store_means(A.out + ((int64_t)seq * A.q_tokens + token) * A.out_stride + head * dim + 8 * unit, f, v, A.P.post);
+}
+
+struct CachePlan {
+    int ct;                           // column tiles of a workgroup
+    int chunks;                       // workgroups over the columns
+    bool whole;                       // one workgroup has all keys
+    int waves;                        // of such a workgroup
+    int32_t split_keys, splits;
+    size_t lds;
+    int64_t pairs, deltas, refs, tops, partial, sums;      // workspace bytes
+};
+
+static int64_t up_to(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+
+static CachePlan plan_of(const CacheAttentionCall &c)
+{
+    CachePlan p;
+    const int columns = c.heads / c.C.kv_heads * c.q_tokens;
+    p.ct = columns > 16 ? 2 : 1;
+    p.chunks = (columns + 16 * p.ct - 1) / (16 * p.ct);
+    p.pairs = (int64_t)c.n_seq * c.C.kv_heads;
+    const int64_t keys = up_to((int64_t)c.max_pages * c.C.page_tokens, 256);
+    const size_t base = (size_t)p.ct * (32 + c.C.dim / 32 * 512) * 4;
+    const size_t scores = (size_t)keys * 16 * p.ct * 2 + (size_t)keys / kTile * 16 * p.ct * 4;
+    p.whole = keys <= 1024;
+    p.waves = keys <= 256 ? 4 : 8;
+    p.split_keys = p.whole ? (int32_t)keys : keys <= 32768 ? 256 : keys <= 65536 ? 512 : 1024;
+    if (p.split_keys == 0) p.split_keys = 256;
+    p.splits = p.whole ? 1 : (int32_t)((keys + p.split_keys - 1) / p.split_keys);
+    p.lds = base + (p.whole ? scores : 0);
+    const int64_t rows = p.whole ? 0 : p.pairs * p.splits * columns, tiles = p.split_keys / kTile;
+    p.deltas = rows * p.split_keys * 2;
+    p.refs = up_to(rows * tiles * 4, 16);
+    p.tops = up_to(rows * 4, 16);
+    p.partial = rows * c.C.dim * 4;
+    p.sums = up_to(rows * 4, 16);
+    return p;
+}
+
+int64_t attention_cache_i4_workspace_bytes(const CacheAttentionCall &c)
+{
+    const CachePlan p = plan_of(c);
+    return p.deltas + p.refs + p.tops + p.partial + p.sums;
+}
+
+static hipError_t launch(const CacheAttentionArgs &a, int ct, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream)
+{
+    switch (a.C.dim) {
+    case 32: return attention_cache_i4_launch_32(a, ct, phases, grid, block, lds, stream);
+    case 64: return attention_cache_i4_launch_64(a, ct, phases, grid, block, lds, stream);
+    case 96: return attention_cache_i4_launch_96(a, ct, phases, grid, block, lds, stream);
+    default: return attention_cache_i4_launch_128(a, ct, phases, grid, block, lds, stream);
+    }
+}
+
+hipError_t attention_cache_i4_dispatch(const CacheAttentionCall &c, hipStream_t stream)
+{
+    const CachePlan p = plan_of(c);
+    CacheAttentionArgs a;
+    a.q = c.q; a.out = c.out; a.q_stride = c.q_stride; a.out_stride = c.out_stride;
+    a.pages = c.pages; a.lengths = c.lengths; a.max_pages = c.max_pages; a.q_tokens = c.q_tokens;
+    a.group = c.heads / c.C.kv_heads;
+    a.columns = a.group * c.q_tokens;
+    a.by_group = div_of((uint32_t)a.group);
+    a.by_kv_heads = div_of((uint32_t)c.C.kv_heads);
+    a.by_chunks = div_of((uint32_t)p.chunks);
+    a.by_splits = div_of((uint32_t)p.splits);
+    a.split_keys = p.split_keys; a.splits = p.splits;
+    char *w = static_cast<char *>(c.work);
+    a.deltas = reinterpret_cast<int16_t *>(w); w += p.deltas;
+    a.partial = reinterpret_cast<int32_t *>(w); w += p.partial;
+    a.refs = reinterpret_cast<int32_t *>(w); w += p.refs;
+    a.tops = reinterpret_cast<int32_t *>(w); w += p.tops;
+    a.sums = reinterpret_cast<uint32_t *>(w);
+    a.C = c.C; a.P = c.P;
+    const uint32_t grid = (uint32_t)(p.pairs * p.chunks * p.splits);
+    if (p.whole) return launch(a, p.ct, 3, grid, 64u * p.waves, p.lds, stream);
+    hipError_t e = launch(a, p.ct, 1, grid, 64u * kSplitWaves, p.lds, stream);
+    if (e != hipSuccess) return e;
+    e = launch(a, p.ct, 2, grid, 64u * kSplitWaves, p.lds, stream);
+    if (e != hipSuccess) return e;
+    a.by_chunks = div_of((uint32_t)a.columns);
+    a.by_splits = div_of((uint32_t)a.split_keys);
+    launch_kernel(attention_cache_i4_join_kernel, dim3((uint32_t)(p.pairs * a.columns)), dim3(256), 0, stream, a);
+    return take_launch_status();
+}
+
+}  // namespace iptq
