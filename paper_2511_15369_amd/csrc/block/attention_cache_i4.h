@@ -26,7 +26,6 @@
 namespace iptq {
 
 constexpr int kTile = 64;             // keys
-constexpr int kSplitWaves = 4;        // wavefronts of a workgroup where the keys are split over workgroups
 
 struct CacheAttentionArgs {
     const int8_t *q;
@@ -35,9 +34,12 @@ struct CacheAttentionArgs {
     const int32_t *pages, *lengths;
     int32_t max_pages, q_tokens, group, columns;          // columns = group * q_tokens
     DivDev by_group, by_kv_heads, by_chunks, by_splits;   // column -> token; workgroup -> kv head, columns, split, sequence
-    int32_t split_keys, splits;                           // keys of a workgroup (a multiple of 256), workgroups a sequence
+    DivDev by_split_keys, by_columns;
+    int32_t column_tiles;                                 // 1 or 2: of a workgroup
+    int32_t split_keys, splits;                           // keys of a workgroup, workgroups over a sequence
+    int32_t wave_keys;                                    // of a wavefront, a multiple of 64 up to 1024
     // between the phases: in LDS where one workgroup has all keys of a sequence, else here
-    int16_t *deltas;                                      // [sequence, kv head][tile, p][column][16]
+    int16_t *deltas;                                      // [sequence, kv head][tile, p][2][column][8]
     int32_t *refs;                                        // [sequence, kv head][tile][column]
     int32_t *tops;                                        // [sequence, kv head][split][column]
     int32_t *partial;                                     // [sequence, kv head][split][column][head_dim]
@@ -63,95 +65,128 @@ IPTQ_DEV i32x4 in_nibble_order(i32x4 v)               // 16 channels of a query 
 IPTQ_DEV int32_t byte_of(const u32x4 *v, int i) { return (int32_t)(v[i >> 4][i >> 2 & 3] >> (8 * (i & 3)) & 255u); }
 
 // PHASES 3: both, scores in LDS; 1: keys only; 2: values only.
-// CT: column tiles of a workgroup.
-template <int D, int VARIANT, int CT, int PHASES>
+// HALVES 2: up to eight queries share a kv head.  The second product's sixteen columns are then the upper halves of
+// eight queries' weights and the lower halves of the same: one product in place of two, and lanes that would have
+// been idle make the same weights as their neighbours.
+// HALVES 1: sixteen queries, one product for either half.
+template <int D, int VARIANT, int HALVES, int PHASES>
 struct CacheAttention {
     static constexpr int G = (D + kGroup - 1) / kGroup, PAIRS = D / 2, BLOCKS = D / 32;    // blocks of 16 channel pairs
+    static constexpr int QUERIES = 16 / HALVES, PRODUCTS = 3 - HALVES;
     static constexpr int ACC = BLOCKS * 2 * 4 * 64;       // sums of one column tile
 
-    struct Keys { u32x2_t codes[4][G]; u32x4 steps[G]; int32_t page; };
+    // A tile's codes as the wavefront loads them, 16 bytes a lane in the order of the memory (a quarter of a
+    // wavefront-wide load then meets whole lines; loaded in the products' order, every lane of a quad had a line of its own
+    // and the L1 took four times the cycles).  They change places in LDS, in a buffer of the wavefront's own.
+    struct Keys { u32x4 codes[BLOCKS]; u32x4 steps[G]; int32_t page; };
     struct Values { u32x4 codes[BLOCKS]; u32x4 steps[G]; };
+    static constexpr int kValueBlock = 4 * 288;           // 16 pairs: four blocks of 256 bytes, 32 apart for the banks' sake
+    static constexpr int STAGE = BLOCKS * kValueBlock > kTile * PAIRS + 256 ? BLOCKS * kValueBlock : kTile * PAIRS + 256;
+    // Where a 16-key block of either starts in the buffer: shifted against each other so that a read's lanes meet all banks.
+    static IPTQ_DEV int keys_at(int block)
+    {
+        return block * 16 * PAIRS + (BLOCKS >= 3 ? 16 * block : BLOCKS == 2 ? 16 * (block & 1) + 128 * (block >> 1) : 64 * block);
+    }
 
     const CacheAttentionArgs &A;
     const int lane, col, p;
-    uint32_t kvh, seq, e0;
-    int32_t length, from, to;                             // keys [from, to) of the workgroup
-    const int32_t *table;
-    i32x4 q[CT][G];
-    int32_t limit[CT], least;                             // keys that a column sees, that all of them see
-    uint32_t e[CT];
+    int8_t *stage;
+    uint32_t kvh, seq, e;
+    int32_t length, limit;                                // keys of the sequence, keys that the lane's query sees
+    int32_t from, to;                                     // the wavefront's keys, at most 1024
+    int32_t page_of_block;                                // lane l: page of the wavefront's block l, or -1
+    i32x4 q[G];
 
-    IPTQ_DEV CacheAttention(const CacheAttentionArgs &a, uint32_t kvh_, uint32_t seq_, uint32_t chunk, uint32_t split)
-        : A(a), lane(threadIdx.x & 63), col(lane & 15), p(lane >> 4), kvh(kvh_), seq(seq_), e0(chunk * 16 * CT)
+    IPTQ_DEV CacheAttention(const CacheAttentionArgs &a, uint32_t kvh_, uint32_t seq_, uint32_t e0, int32_t from_, int32_t keys, int8_t *stage_)
+        : A(a), lane(threadIdx.x & 63), col(lane & 15), p(lane >> 4), stage(stage_), kvh(kvh_), seq(seq_), from(from_)
     {
-        length = min(max(A.lengths[seq], 0), A.max_pages << A.C.page_log);
-        from = (int32_t)split * A.split_keys;
-        to = min(length, from + A.split_keys);
-        table = A.pages + (int64_t)seq * A.max_pages;
-        least = A.P.causal ? length - (A.q_tokens - 1) : length;
+        // the table's entries do not wait for the length: they are looked up inside the table and judged afterwards
+        const int32_t capacity = A.max_pages << A.C.page_log, key = from + 16 * lane;
+        const int32_t page = key < capacity ? (A.pages + (int64_t)seq * A.max_pages)[key >> A.C.page_log] : -1;
+        length = min(max(A.lengths[seq], 0), capacity);
+        to = min(length, from + keys);
+        e = min(e0 + (col & (QUERIES - 1)), (uint32_t)A.columns - 1);     // columns past the last repeat it
+        page_of_block = key < to && page >= 0 && page < A.C.n_pages ? page : -1;
     }
+    IPTQ_DEV uint32_t token() const { return div_by(e, A.by_group); }
     IPTQ_DEV int64_t q_row(uint32_t token) const { return (int64_t)seq * A.q_tokens + token; }
     IPTQ_DEV void load_queries()
     {
+        const uint32_t t = token(), head = kvh * (uint32_t)A.group + (e - t * (uint32_t)A.group);
+        limit = A.P.causal ? length - (A.q_tokens - 1 - (int32_t)t) : length;
+        const int8_t *src = A.q + q_row(t) * A.q_stride + head * D + 16 * p;
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            e[c] = min(e0 + 16 * c + col, (uint32_t)A.columns - 1);       // columns past the last repeat it
-            const uint32_t token = div_by(e[c], A.by_group), head = kvh * (uint32_t)A.group + (e[c] - token * (uint32_t)A.group);
-            limit[c] = A.P.causal ? length - (A.q_tokens - 1 - (int32_t)token) : length;
-            const int8_t *src = A.q + q_row(token) * A.q_stride + head * D + 16 * p;
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                q[c][g] = (i32x4){0, 0, 0, 0};
-                if (kGroup * g + 16 * p < D) q[c][g] = in_nibble_order(*reinterpret_cast<const i32x4_any *>(src + kGroup * g));
-            }
+        for (int g = 0; g < G; ++g) {
+            q[g] = (i32x4){0, 0, 0, 0};
+            if (kGroup * g + 16 * p < D) q[g] = in_nibble_order(*reinterpret_cast<const i32x4_any *>(src + kGroup * g));
         }
     }
-    IPTQ_DEV int32_t page_of(int32_t key) const { return page_of_key(table, A.C.page_log, A.C.n_pages, key, length); }
-
     // Keys [at, at + 64): a page that is not there reads the cache's first one, and is masked.
     IPTQ_DEV Keys load_keys(int32_t at) const
     {
         Keys k;
         const CacheDev &C = A.C;
-        const int32_t mine = at + 16 * p, theirs = at + 16 * (col >> 2);   // the block of the lane's scores; of the keys it loads
-        const int32_t key_page = page_of(theirs);
-        k.page = page_of(mine);
-        const int64_t key_row = ((int64_t)max(key_page, 0) * C.kv_heads + kvh) * C.page_tokens + (theirs & (C.page_tokens - 1)) + (col & 3);
-        const int64_t step_row = ((int64_t)max(k.page, 0) * C.kv_heads + kvh) * C.page_tokens + (mine & (C.page_tokens - 1));
-        const uint8_t *src = C.k_codes + key_row * PAIRS + 8 * p;
+        const int first = (at - from) >> 4, mask = C.page_tokens - 1;
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                k.codes[s][g] = (u32x2_t){0, 0};
-                if (kGroup * g + 16 * p < D) k.codes[s][g] = *reinterpret_cast<const u32x2_t *>(src + 4 * s * PAIRS + kGroup / 2 * g);
-            }
+        for (int i = 0; i < BLOCKS; ++i) {                // (a key's row is BLOCKS chunks of 16 bytes)
+            const int chunk = 64 * i + lane, block = chunk / (16 * BLOCKS), in_block = chunk - block * 16 * BLOCKS;
+            const int32_t page = max(__shfl(page_of_block, first + block), 0);
+            const int64_t row = ((int64_t)page * C.kv_heads + kvh) * C.page_tokens + ((at + 16 * block) & mask);
+            k.codes[i] = *reinterpret_cast<const u32x4 *>(C.k_codes + row * PAIRS + 16 * in_block);
+        }
+        k.page = __shfl(page_of_block, first + p);
+        const int64_t step_row = ((int64_t)max(k.page, 0) * C.kv_heads + kvh) * C.page_tokens + ((at + 16 * p) & mask);
 #pragma unroll
         for (int g = 0; g < G; ++g) k.steps[g] = *reinterpret_cast<const u32x4 *>(C.k_steps + step_row * G + 16 * g);
         return k;
     }
+    IPTQ_DEV void stage_keys(const Keys &k) const
+    {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            const int chunk = 64 * i + lane, block = chunk / (16 * BLOCKS), in_block = chunk - block * 16 * BLOCKS;
+            *reinterpret_cast<u32x4 *>(stage + keys_at(block) + 16 * in_block) = k.codes[i];
+        }
+        wave_lds_fence();
+    }
+    // The block and the channel pair (of 16) whose tokens the lane loads: a page's tokens of a pair lie side by side, so
+    // the lanes of a quad take blocks of the same page and then further pairs.
+    IPTQ_DEV int value_block() const { return A.C.page_log >= 6 ? lane & 3 : A.C.page_log == 5 ? (lane & 1) | lane >> 5 << 1 : lane >> 4; }
+    IPTQ_DEV int value_pair() const { return A.C.page_log >= 6 ? lane >> 2 : A.C.page_log == 5 ? lane >> 1 & 15 : lane & 15; }
     IPTQ_DEV Values load_values(int32_t at) const
     {
         Values v;
         const CacheDev &C = A.C;
-        const int32_t mine = at + 16 * p, pos = mine & (C.page_tokens - 1);
-        const int64_t head_at = (int64_t)max(page_of(mine), 0) * C.kv_heads + kvh;
+        const int first = (at - from) >> 4, mask = C.page_tokens - 1, block = value_block();
+        const int64_t head_at = (int64_t)max(__shfl(page_of_block, first + block), 0) * C.kv_heads + kvh;
+        const uint8_t *src = C.v_codes + (head_at * PAIRS + value_pair()) * C.page_tokens + ((at + 16 * block) & mask);
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b)
-            v.codes[b] = *reinterpret_cast<const u32x4 *>(C.v_codes + (head_at * PAIRS + 16 * b + col) * C.page_tokens + pos);
+        for (int b = 0; b < BLOCKS; ++b) v.codes[b] = *reinterpret_cast<const u32x4 *>(src + (int64_t)(16 * b) * C.page_tokens);
+        const int64_t step_row = ((int64_t)max(__shfl(page_of_block, first + p), 0) * C.kv_heads + kvh) * C.page_tokens + ((at + 16 * p) & mask);
 #pragma unroll
-        for (int g = 0; g < G; ++g) v.steps[g] = *reinterpret_cast<const u32x4 *>(C.v_steps + (head_at * C.page_tokens + pos) * G + 16 * g);
+        for (int g = 0; g < G; ++g) v.steps[g] = *reinterpret_cast<const u32x4 *>(C.v_steps + step_row * G + 16 * g);
         return v;
     }
+    IPTQ_DEV void stage_values(const Values &v) const
+    {
+        const int at = value_block() * 288 + value_pair() * 16;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) *reinterpret_cast<u32x4 *>(stage + b * kValueBlock + at) = v.codes[b];
+        wave_lds_fence();
+    }
     // Scores of a tile -> 16-bit differences from the tile's largest of the column (packed pairs), and that largest.
-    IPTQ_DEV void score(const Keys &k, int32_t at, int c, uint32_t (&d)[8], int32_t *ref) const
+    IPTQ_DEV void score(const Keys &k, int32_t at, uint32_t (&d)[8], int32_t *ref) const
     {
         int32_t x[16];
+        stage_keys(k);
+        const int8_t *src = stage + keys_at(col >> 2) + (col & 3) * PAIRS + 8 * p;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const i32x4 y = __builtin_amdgcn_mfma_i32_16x16x64_i8(upper_nibbles(k.codes[s][g]), q[c][g], (i32x4){0, 0, 0, 0}, 0, 0, 0);
+                // (where the last group is half a one, lanes 32 on take the others' codes, against zeros of the query)
+                const u32x2_t codes = *reinterpret_cast<const u32x2_t *>(src + (kGroup * g + 48 < D ? 0 : p >= 2 ? -16 : 0) + 4 * s * PAIRS + kGroup / 2 * g);
+                const i32x4 y = __builtin_amdgcn_mfma_i32_16x16x64_i8(upper_nibbles(codes), q[g], (i32x4){0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int32_t t = __mul24(byte_of(k.steps, (4 * s + r) * G + g), y[r]);
@@ -159,9 +194,10 @@ struct CacheAttention {
                 }
             }
         }
+        wave_lds_fence();                                 // the buffer may be written again
         // scores are 16 times their value: a shift of four more
         const int32_t shift = A.P.shift + 4, rounding = A.P.shift > 0 ? 1 << (shift - 1) : 0;
-        const int32_t seen = k.page >= 0 ? limit[c] - (at + 16 * p) : 0;      // of the lane's 16 keys
+        const int32_t seen = k.page >= 0 ? limit - (at + 16 * p) : 0;         // of the lane's 16 keys
         const bool whole = __all(seen >= 16);
         int32_t top = kI32Min;
         if (whole) {
@@ -184,15 +220,17 @@ struct CacheAttention {
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pk_i16(x[2 * i], x[2 * i + 1]));
     }
-    // One tile's share of the weighted values of a column tile.
-    IPTQ_DEV void accumulate(const Values &v, const uint32_t (&d)[8], int32_t ref, int32_t top, i32x4 (&acc)[BLOCKS][2][2], uint32_t *sum) const
+    // One tile's share of the weighted values.
+    IPTQ_DEV void accumulate(const Values &v, const uint32_t (&d)[8], int32_t ref, int32_t top, i32x4 (&acc)[BLOCKS][2][PRODUCTS],
+                             uint32_t *sum) const
     {
+        stage_values(v);
         const short off = (short)(ref == kI32Min ? -32768 : max(ref - top, -32768));
-        const i16x2 least_d = {(short)-A.P.d_clamp, (short)-A.P.d_clamp}, offs = {off, off};
+        const i16x2 least = {(short)-A.P.d_clamp, (short)-A.P.d_clamp}, offs = {off, off};
         uint32_t w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const i16x2 t = __builtin_elementwise_max(__builtin_elementwise_add_sat(__builtin_bit_cast(i16x2, d[i]), offs), least_d);
+            const i16x2 t = __builtin_elementwise_max(__builtin_elementwise_add_sat(__builtin_bit_cast(i16x2, d[i]), offs), least);
             w[i] = weights_of_pair<VARIANT>(t, A.P);
             *sum = __builtin_amdgcn_udot2(__builtin_bit_cast(u16x2_t, w[i]), (u16x2_t){1, 1}, *sum, false);
         }
@@ -213,16 +251,21 @@ struct CacheAttention {
                 split_weights(u[0], u[1], &h, &l);
                 hi[g][i] = (int32_t)h;
                 lo[g][i] = (int32_t)l;
+                if (HALVES == 2) hi[g][i] = col < 8 ? hi[g][i] : lo[g][i];
             }
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
             const int g = 32 * b / kGroup;
-            const i32x4 even = __builtin_bit_cast(i32x4, v.codes[b] << 4 & 0xf0f0f0f0u), odd = __builtin_bit_cast(i32x4, v.codes[b] & 0xf0f0f0f0u);
+            const u32x4 codes = *reinterpret_cast<const u32x4 *>(stage + b * kValueBlock + p * 288 + col * 16);
+            const i32x4 even = __builtin_bit_cast(i32x4, codes << 4 & 0xf0f0f0f0u), odd = __builtin_bit_cast(i32x4, codes & 0xf0f0f0f0u);
             acc[b][0][0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(even, hi[g], acc[b][0][0], 0, 0, 0);
-            acc[b][0][1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(even, lo[g], acc[b][0][1], 0, 0, 0);
             acc[b][1][0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(odd, hi[g], acc[b][1][0], 0, 0, 0);
-            acc[b][1][1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(odd, lo[g], acc[b][1][1], 0, 0, 0);
+            if (HALVES == 1) {
+                acc[b][0][PRODUCTS - 1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(even, lo[g], acc[b][0][PRODUCTS - 1], 0, 0, 0);
+                acc[b][1][PRODUCTS - 1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(odd, lo[g], acc[b][1][PRODUCTS - 1], 0, 0, 0);
+            }
         }
+        wave_lds_fence();                                 // the buffer may be written again
     }
 };
 
@@ -236,135 +279,136 @@ IPTQ_DEV void store_means(int8_t *out, uint64_t f, const int64_t (&acc)[8], cons
     *reinterpret_cast<u32x2_any *>(out) = (u32x2_t){w[0], w[1]};
 }
 
-// LDS: [tops 16 CT][sums 16 CT] then the sums [CT][ACC], and (PHASES 3) deltas [tiles * 4][16 CT][16] and
-// refs [tiles][16 CT].
-template <int D, int VARIANT, int CT, int PHASES>
+// A workgroup's wavefronts: A.column_tiles of them side by side over the columns, the others over the keys.
+// LDS: a staging buffer per wavefront; per column tile [tops 16], [sums 16] and the sums [ACC]; (PHASES 3) deltas
+// [tiles * 4][2][queries][8] and refs [tiles][queries] with the queries of all column tiles.
+template <int D, int VARIANT, int HALVES, int PHASES>
 IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, uint32_t seq, uint32_t chunk, uint32_t split)
 {
-    typedef CacheAttention<D, VARIANT, CT, PHASES> T;
-    extern __shared__ __attribute__((aligned(16))) int32_t lds[];
-    int32_t *lds_top = lds, *lds_acc = lds + 32 * CT;
-    uint32_t *lds_sum = reinterpret_cast<uint32_t *>(lds + 16 * CT);
-    T t(A, kvh, seq, chunk, split);
-    const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = t.lane, col = t.col, p = t.p;
-    if (PHASES != 3 && t.from >= t.to) return;            // no key in this split
+    typedef CacheAttention<D, VARIANT, HALVES, PHASES> T;
+    extern __shared__ __attribute__((aligned(16))) int8_t lds_bytes[];
+    const int ct = A.column_tiles, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int key_wave = ct == 2 ? wave >> 1 : wave, c = ct == 2 ? wave & 1 : 0;
+    int32_t *lds = reinterpret_cast<int32_t *>(lds_bytes + (blockDim.x >> 6) * T::STAGE);
+    int32_t *lds_top = lds + 16 * c, *lds_acc = lds + 32 * ct + c * T::ACC;
+    uint32_t *lds_sum = reinterpret_cast<uint32_t *>(lds + 16 * ct + 16 * c);
+    const int e_wg = (int)chunk * T::QUERIES * ct;                         // the workgroup's first query
+    T t(A, kvh, seq, (uint32_t)(e_wg + T::QUERIES * c), (int32_t)split * A.split_keys + key_wave * A.wave_keys, A.wave_keys,
+        lds_bytes + wave * T::STAGE);
+    const int lane = t.lane, col = t.col, p = t.p;
+    if (PHASES != 3 && (int32_t)split * A.split_keys >= t.length) return; // no key in this split
     t.load_queries();
     const int64_t pair = (int64_t)seq * A.C.kv_heads + kvh;
     const int32_t tiles = (A.split_keys * A.splits) / kTile;               // of a sequence's share of the workspace
-    const int columns = PHASES == 3 ? 16 * CT : A.columns;
-    int16_t *deltas = PHASES == 3 ? reinterpret_cast<int16_t *>(lds_acc + CT * T::ACC) : A.deltas + pair * tiles * 4 * columns * 16;
-    int32_t *refs = PHASES == 3 ? lds_acc + CT * T::ACC + tiles * 4 * 16 * CT * 8 : A.refs + pair * tiles * columns;
-    const int e0 = PHASES == 3 ? 0 : (int)t.e0;
-    bool mine[CT];                                        // whether the column is one of the workspace's
-#pragma unroll
-    for (int c = 0; c < CT; ++c) mine[c] = PHASES == 3 || e0 + 16 * c + col < columns;
+    const int columns = PHASES == 3 ? T::QUERIES * ct : A.columns;
+    int16_t *deltas = PHASES == 3 ? reinterpret_cast<int16_t *>(lds + (32 + T::ACC) * ct) : A.deltas + pair * tiles * 4 * columns * 16;
+    int32_t *refs = PHASES == 3 ? lds + (32 + T::ACC) * ct + tiles * 4 * columns * 8 : A.refs + pair * tiles * columns;
+    const int column = (PHASES == 3 ? 0 : e_wg) + T::QUERIES * c + (col & (T::QUERIES - 1));
+    const bool mine = col < T::QUERIES && column < columns;                // the lane writes its column's scores
 
-    const int32_t first = t.from + kTile * wave, step = kTile * waves;
-    int32_t top[CT];
-#pragma unroll
-    for (int c = 0; c < CT; ++c) top[c] = kI32Min;
-    if (threadIdx.x < 16 * CT) lds_top[threadIdx.x] = kI32Min;
+    int32_t top = kI32Min;
+    if (threadIdx.x < 16 * (unsigned)ct) lds[threadIdx.x] = kI32Min;
     if (PHASES & 2)
-        for (int i = threadIdx.x; i < 16 * CT + CT * T::ACC; i += blockDim.x) lds[16 * CT + i] = 0;       // sums
-    __syncthreads();
+        for (int i = threadIdx.x; i < (16 + T::ACC) * ct; i += blockDim.x) lds[16 * ct + i] = 0;           // sums
     if (PHASES & 1) {
-        if (first < t.to) {
-            typename T::Keys now = t.load_keys(first);
-            for (int32_t at = first; at < t.to; at += step) {
-                const typename T::Keys next = t.load_keys(min(at + step, t.to - 1) & ~(kTile - 1));
-#pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    uint32_t d[8];
-                    int32_t ref;
-                    t.score(now, at, c, d, &ref);
-                    top[c] = max(top[c], ref);
-                    const int32_t tile = at / kTile;
-                    if (mine[c]) {
-                        u32x4 *o = reinterpret_cast<u32x4 *>(deltas + ((int64_t)(tile * 4 + p) * columns + e0 + 16 * c + col) * 16);
-                        o[0] = (u32x4){d[0], d[1], d[2], d[3]};
-                        o[1] = (u32x4){d[4], d[5], d[6], d[7]};
-                        if (p == 0) refs[tile * columns + e0 + 16 * c + col] = ref;
-                    }
+        if (t.from < t.to) {
+            typename T::Keys now = t.load_keys(t.from);
+            for (int32_t at = t.from; at < t.to; at += kTile) {
+                const typename T::Keys next = t.load_keys(min(at + kTile, (t.to - 1) & ~(kTile - 1)));
+                uint32_t d[8];
+                int32_t ref;
+                t.score(now, at, d, &ref);
+                top = max(top, ref);
+                const int32_t tile = at / kTile;
+                if (mine) {
+                    u32x4 *o = reinterpret_cast<u32x4 *>(deltas) + (int64_t)(tile * 4 + p) * 2 * columns + column;
+                    o[0] = (u32x4){d[0], d[1], d[2], d[3]};
+                    o[columns] = (u32x4){d[4], d[5], d[6], d[7]};
+                    if (p == 0) refs[tile * columns + column] = ref;
                 }
                 now = next;
             }
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-                if (p == 0) atomicMax(lds_top + 16 * c + col, top[c]);
         }
+        __syncthreads();
+        if (p == 0 && t.from < t.to) atomicMax(lds_top + col, top);
         __syncthreads();
         if (PHASES == 1) {
-            const int i = threadIdx.x;
-            if (i < 16 * CT && e0 + i < columns) A.tops[(pair * A.splits + split) * columns + e0 + i] = lds_top[i];
+            const int i = threadIdx.x, j = i & (T::QUERIES - 1), cc = i / T::QUERIES;
+            if (cc < ct && e_wg + i < columns) A.tops[(pair * A.splits + split) * columns + e_wg + i] = lds[16 * cc + j];
             return;
         }
+    } else {
+        __syncthreads();
     }
     if (PHASES == 2) {                                    // the largest score of all splits that have keys
-        const int32_t live = (t.length + A.split_keys - 1) / A.split_keys;
-        for (int i = threadIdx.x; i < live * 16 * CT; i += blockDim.x) {
-            const int c = i % (16 * CT);
-            if (e0 + c < columns) atomicMax(lds_top + c, A.tops[(pair * A.splits + i / (16 * CT)) * columns + e0 + c]);
+        const int32_t live = div_by((uint32_t)(t.length + A.split_keys - 1), A.by_split_keys);
+        const int log = ct == 2 ? 5 : 4;
+        for (int i = threadIdx.x & (16 * ct - 1), s = threadIdx.x >> log; s < live; s += blockDim.x >> log) {
+            const int j = i & 15, x = e_wg + (i >> 4) * T::QUERIES + (j & (T::QUERIES - 1));
+            if (x < columns) atomicMax(lds + i, A.tops[(pair * A.splits + s) * columns + x]);
         }
         __syncthreads();
     }
-#pragma unroll
-    for (int c = 0; c < CT; ++c) top[c] = lds_top[16 * c + col];
+    top = lds_top[col];
 
-    if (first < t.to) {
-        i32x4 acc[CT][T::BLOCKS][2][2];
-        uint32_t sum[CT];
+    if (t.from < t.to) {
+        i32x4 acc[T::BLOCKS][2][T::PRODUCTS];
+        uint32_t sum = 0;
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            sum[c] = 0;
+        for (int b = 0; b < T::BLOCKS; ++b)
 #pragma unroll
-            for (int b = 0; b < T::BLOCKS; ++b)
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int n = 0; n < 4; ++n) acc[c][b][n >> 1][n & 1] = (i32x4){0, 0, 0, 0};
-        }
-        typename T::Values now = t.load_values(first);
-        for (int32_t at = first; at < t.to; at += step) {
-            const typename T::Values next = t.load_values(min(at + step, t.to - 1) & ~(kTile - 1));
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                const int32_t tile = at / kTile, column = mine[c] ? e0 + 16 * c + col : columns - 1;
-                const u32x4 *o = reinterpret_cast<const u32x4 *>(deltas + ((int64_t)(tile * 4 + p) * columns + column) * 16);
-                const u32x4 a = o[0], b = o[1];
-                const uint32_t d[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-                t.accumulate(now, d, refs[tile * columns + column], top[c], acc[c], &sum[c]);
-            }
+                for (int h = 0; h < T::PRODUCTS; ++h) acc[b][n][h] = (i32x4){0, 0, 0, 0};
+        const int from_column = min(column, columns - 1);
+        struct Scores { u32x4 a, b; int32_t ref; };
+        auto load_scores = [&](int32_t at) {
+            const u32x4 *o = reinterpret_cast<const u32x4 *>(deltas) + (int64_t)(at / kTile * 4 + p) * 2 * columns + from_column;
+            return (Scores){o[0], o[columns], refs[at / kTile * columns + from_column]};
+        };
+        typename T::Values now = t.load_values(t.from);
+        Scores scores = load_scores(t.from);
+        for (int32_t at = t.from; at < t.to; at += kTile) {
+            const int32_t ahead = min(at + kTile, (t.to - 1) & ~(kTile - 1));
+            const typename T::Values next = t.load_values(ahead);
+            const Scores further = load_scores(ahead);
+            const uint32_t d[8] = {scores.a.x, scores.a.y, scores.a.z, scores.a.w, scores.b.x, scores.b.y, scores.b.z, scores.b.w};
+            t.accumulate(now, d, scores.ref, top, acc, &sum);
             now = next;
+            scores = further;
         }
         // the wavefronts' sums: whole numbers, so the order in which they are added does not matter
+        sum += (uint32_t)__shfl_xor((int32_t)sum, 16);
+        sum += (uint32_t)__shfl_xor((int32_t)sum, 32);
+        if (p == 0) atomicAdd(lds_sum + col, sum);
+        // 16 (256 hi + lo) of either half; HALVES 2: of the half that the lane's column is
+        const int up = HALVES == 2 && col >= 8 ? 0 : 8;
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            sum[c] += (uint32_t)__shfl_xor((int32_t)sum[c], 16);
-            sum[c] += (uint32_t)__shfl_xor((int32_t)sum[c], 32);
-            if (p == 0) atomicAdd(lds_sum + 16 * c + col, sum[c]);
+        for (int b = 0; b < T::BLOCKS; ++b)
 #pragma unroll
-            for (int b = 0; b < T::BLOCKS; ++b)
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        atomicAdd(lds_acc + c * T::ACC + ((b * 2 + n) * 4 + r) * 64 + lane, acc[c][b][n][0][r] * 16 + (acc[c][b][n][1][r] >> 4));
-        }
+                for (int r = 0; r < 4; ++r) {
+                    int32_t v = HALVES == 2 ? acc[b][n][0][r] >> 4 << up : acc[b][n][0][r] * 16 + (acc[b][n][T::PRODUCTS - 1][r] >> 4);
+                    atomicAdd(lds_acc + ((b * 2 + n) * 4 + r) * 64 + (HALVES == 2 ? lane & ~8 : lane), v);
+                }
     }
     __syncthreads();
     // a thread's block of 16 channel pairs and lane: rows 4 p + r are the pairs 16 b + 4 p + r, eight channels in a row
-    for (int u = threadIdx.x; u < CT * T::BLOCKS * 64; u += blockDim.x) {
-        const int c = u / (T::BLOCKS * 64), b = (u >> 6) % T::BLOCKS, l = u & 63;
-        const uint32_t column = t.e0 + 16 * c + (l & 15);
-        if (column >= (uint32_t)A.columns) continue;
+    for (int u = threadIdx.x; u < ct * T::BLOCKS * 64; u += blockDim.x) {
+        const int cc = u / (T::BLOCKS * 64), b = (u >> 6) % T::BLOCKS, l = u & 63, j = l & 15;
+        const uint32_t x = (uint32_t)(e_wg + T::QUERIES * cc + j);
+        if (j >= T::QUERIES || x >= (uint32_t)A.columns) continue;
         int64_t v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = lds_acc[c * T::ACC + ((b * 2 + (i & 1)) * 4 + (i >> 1)) * 64 + l];
-        const uint32_t s = lds_sum[16 * c + (l & 15)];
+        for (int i = 0; i < 8; ++i) v[i] = lds[32 * ct + cc * T::ACC + ((b * 2 + (i & 1)) * 4 + (i >> 1)) * 64 + l];
+        const uint32_t s = (uint32_t)lds[16 * ct + 16 * cc + j];
         const int channel = 32 * b + 8 * (l >> 4);
         if (PHASES == 3) {
-            const uint32_t token = div_by(column, A.by_group), head = kvh * (uint32_t)A.group + (column - token * (uint32_t)A.group);
+            const uint32_t token = div_by(x, A.by_group), head = kvh * (uint32_t)A.group + (x - token * (uint32_t)A.group);
             store_means(A.out + t.q_row(token) * A.out_stride + head * D + channel, floor_div_u64((uint64_t)1 << 54, s), v, A.P.post);
         } else {
-            const int64_t at = (pair * A.splits + split) * A.columns + column;
+            const int64_t at = (pair * A.splits + split) * A.columns + x;
             i32x4 *o = reinterpret_cast<i32x4 *>(A.partial + at * D + channel);
             o[0] = (i32x4){(int32_t)v[0], (int32_t)v[1], (int32_t)v[2], (int32_t)v[3]};
             o[1] = (i32x4){(int32_t)v[4], (int32_t)v[5], (int32_t)v[6], (int32_t)v[7]};
@@ -373,37 +417,37 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
     }
 }
 
-template <int D, int VARIANT, int CT, int PHASES>
-__global__ __launch_bounds__(PHASES == 3 ? 512 : 256) void attention_cache_i4_kernel(const CacheAttentionArgs A)
+template <int D, int VARIANT, int HALVES, int PHASES>
+__global__ __launch_bounds__(512) void attention_cache_i4_kernel(const CacheAttentionArgs A)
 {
     const uint32_t r1 = div_by(blockIdx.x, A.by_kv_heads), kvh = blockIdx.x - r1 * A.by_kv_heads.d;
     const uint32_t r2 = div_by(r1, A.by_chunks), chunk = r1 - r2 * A.by_chunks.d;
     const uint32_t seq = div_by(r2, A.by_splits), split = r2 - seq * A.by_splits.d;
-    cache_attention_body<D, VARIANT, CT, PHASES>(A, kvh, seq, chunk, split);
+    cache_attention_body<D, VARIANT, HALVES, PHASES>(A, kvh, seq, chunk, split);
 }
 
-hipError_t attention_cache_i4_launch_32(const CacheAttentionArgs &a, int ct, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream);
-hipError_t attention_cache_i4_launch_64(const CacheAttentionArgs &a, int ct, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream);
-hipError_t attention_cache_i4_launch_96(const CacheAttentionArgs &a, int ct, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream);
-hipError_t attention_cache_i4_launch_128(const CacheAttentionArgs &a, int ct, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream);
+hipError_t attention_cache_i4_launch_32(const CacheAttentionArgs &a, int halves, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream);
+hipError_t attention_cache_i4_launch_64(const CacheAttentionArgs &a, int halves, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream);
+hipError_t attention_cache_i4_launch_96(const CacheAttentionArgs &a, int halves, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream);
+hipError_t attention_cache_i4_launch_128(const CacheAttentionArgs &a, int halves, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream);
 
 // One file per head dimension instantiates its kernels.
 template <int D, int VARIANT>
-hipError_t attention_cache_i4_launch_of(const CacheAttentionArgs &a, int ct, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream)
+hipError_t attention_cache_i4_launch_of(const CacheAttentionArgs &a, int halves, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream)
 {
-    auto kernel = phases == 3 ? (ct == 1 ? attention_cache_i4_kernel<D, VARIANT, 1, 3> : attention_cache_i4_kernel<D, VARIANT, 2, 3>)
-                  : phases == 2 ? (ct == 1 ? attention_cache_i4_kernel<D, VARIANT, 1, 2> : attention_cache_i4_kernel<D, VARIANT, 2, 2>)
-                  : ct == 1 ? attention_cache_i4_kernel<D, 0, 1, 1> : attention_cache_i4_kernel<D, 0, 2, 1>;
+    auto kernel = phases == 3 ? (halves == 1 ? attention_cache_i4_kernel<D, VARIANT, 1, 3> : attention_cache_i4_kernel<D, VARIANT, 2, 3>)
+                  : phases == 2 ? (halves == 1 ? attention_cache_i4_kernel<D, VARIANT, 1, 2> : attention_cache_i4_kernel<D, VARIANT, 2, 2>)
+                  : halves == 1 ? attention_cache_i4_kernel<D, 0, 1, 1> : attention_cache_i4_kernel<D, 0, 2, 1>;
     launch_kernel(kernel, dim3(grid), dim3(block), lds, stream, a);
     return take_launch_status();
 }
 #define IPTQ_ATTENTION_CACHE_I4_OF(D)                                                                                         \
-    hipError_t iptq::attention_cache_i4_launch_##D(const CacheAttentionArgs &a, int ct, int phases, uint32_t grid, uint32_t block, \
+    hipError_t iptq::attention_cache_i4_launch_##D(const CacheAttentionArgs &a, int halves, int phases, uint32_t grid, uint32_t block, \
                                                    size_t lds, hipStream_t stream)                                            \
     {                                                                                                                         \
         return (a.P.variant == 0   ? attention_cache_i4_launch_of<D, 0>                                                       \
                 : a.P.variant == 1 ? attention_cache_i4_launch_of<D, 1>                                                       \
-                                   : attention_cache_i4_launch_of<D, 2>)(a, ct, phases, grid, block, lds, stream);            \
+                                   : attention_cache_i4_launch_of<D, 2>)(a, halves, phases, grid, block, lds, stream);            \
     }
 
 }  // namespace iptq

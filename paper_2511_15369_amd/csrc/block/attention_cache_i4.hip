@@ -1,4 +1,6 @@
 // Attention over the 4-bit cache: how the keys are divided, the launches, and the last one, which adds up the splits.
+#include <algorithm>
+
 #include "attention_cache_i4.h"
 
 namespace iptq {
@@ -8,11 +10,11 @@ __global__ __launch_bounds__(256) void attention_cache_i4_join_kernel(const Cach
 {
     __shared__ int64_t parts[4][16][8];
     __shared__ uint32_t totals[4];
-    const uint32_t pair = div_by(blockIdx.x, A.by_chunks), column = blockIdx.x - pair * A.by_chunks.d;     // by_chunks: columns here
+    const uint32_t pair = div_by(blockIdx.x, A.by_columns), column = blockIdx.x - pair * A.by_columns.d;
     const uint32_t seq = div_by(pair, A.by_kv_heads), kvh = pair - seq * A.by_kv_heads.d;
     const int dim = A.C.dim, unit = threadIdx.x & 15, part = threadIdx.x >> 4, wave = threadIdx.x >> 6;
     const int32_t length = min(max(A.lengths[seq], 0), A.max_pages << A.C.page_log);
-    const int32_t live = (int32_t)div_by((uint32_t)(length + A.split_keys - 1), A.by_splits);              // by_splits: keys here
+    const int32_t live = (int32_t)div_by((uint32_t)(length + A.split_keys - 1), A.by_split_keys);
     int64_t v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     uint32_t s = 0;
     if (8 * unit < dim)
@@ -45,11 +47,10 @@ __global__ __launch_bounds__(256) void attention_cache_i4_join_kernel(const Cach
 }
 
 struct CachePlan {
-    int ct;                           // column tiles of a workgroup
-    int chunks;                       // workgroups over the columns
+    int halves, ct, chunks;           // weights' halves side by side; column tiles of a workgroup; workgroups over the columns
     bool whole;                       // one workgroup has all keys
-    int waves;                        // of such a workgroup
-    int32_t split_keys, splits;
+    int key_waves;                    // of a workgroup
+    int32_t wave_keys, split_keys, splits;
     size_t lds;
     int64_t pairs, deltas, refs, tops, partial, sums;      // workspace bytes
 };
@@ -60,18 +61,26 @@ static CachePlan plan_of(const CacheAttentionCall &c)
 {
     CachePlan p;
     const int columns = c.heads / c.C.kv_heads * c.q_tokens;
+    p.halves = columns <= 8 ? 2 : 1;
     p.ct = columns > 16 ? 2 : 1;
-    p.chunks = (columns + 16 * p.ct - 1) / (16 * p.ct);
+    const int queries = 16 / p.halves * p.ct;
+    p.chunks = (columns + queries - 1) / queries;
     p.pairs = (int64_t)c.n_seq * c.C.kv_heads;
-    const int64_t keys = up_to((int64_t)c.max_pages * c.C.page_tokens, 256);
-    const size_t base = (size_t)p.ct * (32 + c.C.dim / 32 * 512) * 4;
-    const size_t scores = (size_t)keys * 16 * p.ct * 2 + (size_t)keys / kTile * 16 * p.ct * 4;
+    const int64_t keys = std::max<int64_t>(up_to((int64_t)c.max_pages * c.C.page_tokens, kTile), kTile);
     p.whole = keys <= 1024;
-    p.waves = keys <= 256 ? 4 : 8;
-    p.split_keys = p.whole ? (int32_t)keys : keys <= 32768 ? 256 : keys <= 65536 ? 512 : 1024;
-    if (p.split_keys == 0) p.split_keys = 256;
-    p.splits = p.whole ? 1 : (int32_t)((keys + p.split_keys - 1) / p.split_keys);
-    p.lds = base + (p.whole ? scores : 0);
+    p.key_waves = 4;
+    if (p.whole) {
+        p.wave_keys = keys <= 256 ? kTile : (int32_t)up_to(keys, 256) / 4;
+    } else {
+        // workgroups enough for the chip, but no more than the partial sums of each are worth
+        int64_t split = 256;
+        while (split < 4096 && (split < 64 * queries || keys * p.pairs * p.chunks / split > 4096)) split *= 2;
+        p.wave_keys = (int32_t)split / 4;
+    }
+    p.split_keys = p.wave_keys * p.key_waves;
+    p.splits = (int32_t)((keys + p.split_keys - 1) / p.split_keys);
+    const size_t blocks = c.C.dim / 32, stage = std::max(blocks * 4 * 288, (size_t)kTile * c.C.dim / 2 + 256);       // CacheAttention::STAGE
+    p.lds = (size_t)p.key_waves * p.ct * stage + (size_t)p.ct * (32 + c.C.dim / 32 * 512) * 4 + (p.whole ? (size_t)p.split_keys / kTile * queries * (4 * 32 + 4) : 0);
     const int64_t rows = p.whole ? 0 : p.pairs * p.splits * columns, tiles = p.split_keys / kTile;
     p.deltas = rows * p.split_keys * 2;
     p.refs = up_to(rows * tiles * 4, 16);
@@ -87,13 +96,13 @@ int64_t attention_cache_i4_workspace_bytes(const CacheAttentionCall &c)
     return p.deltas + p.refs + p.tops + p.partial + p.sums;
 }
 
-static hipError_t launch(const CacheAttentionArgs &a, int ct, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream)
+static hipError_t launch(const CacheAttentionArgs &a, int halves, int phases, uint32_t grid, uint32_t block, size_t lds, hipStream_t stream)
 {
     switch (a.C.dim) {
-    case 32: return attention_cache_i4_launch_32(a, ct, phases, grid, block, lds, stream);
-    case 64: return attention_cache_i4_launch_64(a, ct, phases, grid, block, lds, stream);
-    case 96: return attention_cache_i4_launch_96(a, ct, phases, grid, block, lds, stream);
-    default: return attention_cache_i4_launch_128(a, ct, phases, grid, block, lds, stream);
+    case 32: return attention_cache_i4_launch_32(a, halves, phases, grid, block, lds, stream);
+    case 64: return attention_cache_i4_launch_64(a, halves, phases, grid, block, lds, stream);
+    case 96: return attention_cache_i4_launch_96(a, halves, phases, grid, block, lds, stream);
+    default: return attention_cache_i4_launch_128(a, halves, phases, grid, block, lds, stream);
     }
 }
 
@@ -109,7 +118,10 @@ hipError_t attention_cache_i4_dispatch(const CacheAttentionCall &c, hipStream_t 
     a.by_kv_heads = div_of((uint32_t)c.C.kv_heads);
     a.by_chunks = div_of((uint32_t)p.chunks);
     a.by_splits = div_of((uint32_t)p.splits);
-    a.split_keys = p.split_keys; a.splits = p.splits;
+    a.by_split_keys = div_of((uint32_t)p.split_keys);
+    a.by_columns = div_of((uint32_t)a.columns);
+    a.column_tiles = p.ct;
+    a.split_keys = p.split_keys; a.splits = p.splits; a.wave_keys = p.wave_keys;
     char *w = static_cast<char *>(c.work);
     a.deltas = reinterpret_cast<int16_t *>(w); w += p.deltas;
     a.partial = reinterpret_cast<int32_t *>(w); w += p.partial;
@@ -118,13 +130,12 @@ hipError_t attention_cache_i4_dispatch(const CacheAttentionCall &c, hipStream_t 
     a.sums = reinterpret_cast<uint32_t *>(w);
     a.C = c.C; a.P = c.P;
     const uint32_t grid = (uint32_t)(p.pairs * p.chunks * p.splits);
-    if (p.whole) return launch(a, p.ct, 3, grid, 64u * p.waves, p.lds, stream);
-    hipError_t e = launch(a, p.ct, 1, grid, 64u * kSplitWaves, p.lds, stream);
+    const uint32_t block = 64u * p.key_waves * p.ct;
+    if (p.whole) return launch(a, p.halves, 3, grid, block, p.lds, stream);
+    hipError_t e = launch(a, p.halves, 1, grid, block, p.lds, stream);
     if (e != hipSuccess) return e;
-    e = launch(a, p.ct, 2, grid, 64u * kSplitWaves, p.lds, stream);
+    e = launch(a, p.halves, 2, grid, block, p.lds, stream);
     if (e != hipSuccess) return e;
-    a.by_chunks = div_of((uint32_t)a.columns);
-    a.by_splits = div_of((uint32_t)a.split_keys);
     launch_kernel(attention_cache_i4_join_kernel, dim3((uint32_t)(p.pairs * a.columns)), dim3(256), 0, stream, a);
     return take_launch_status();
 }
