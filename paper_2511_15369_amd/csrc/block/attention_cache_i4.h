@@ -34,10 +34,9 @@ struct CacheAttentionArgs {
     const int32_t *pages, *lengths;
     int32_t max_pages, q_tokens, group, columns;          // columns = group * q_tokens
     DivDev by_group, by_kv_heads, by_chunks, by_splits;   // column -> token; workgroup -> kv head, columns, split, sequence
-    DivDev by_split_keys, by_columns;
-    int32_t column_tiles;                                 // 1 or 2: of a workgroup
-    int32_t split_keys, splits;                           // keys of a workgroup, workgroups over a sequence
-    int32_t wave_keys;                                    // of a wavefront, a multiple of 64 up to 1024
+    DivDev by_span, by_columns;                           // span: 64 keys of each wavefront that a sequence's keys are divided over
+    int32_t column_tiles, key_waves;                      // of a workgroup: wavefronts side by side over the columns (1 or 2), over the keys
+    int32_t splits, tiles;                                // workgroups over a sequence; tiles of the workspace a sequence
     // between the phases: in LDS where one workgroup has all keys of a sequence, else here
     int16_t *deltas;                                      // [sequence, kv head][tile, p][2][column][8]
     int32_t *refs;                                        // [sequence, kv head][tile][column]
@@ -47,6 +46,17 @@ struct CacheAttentionArgs {
     CacheDev C;
     AttentionDev P;
 };
+
+// Keys of a wavefront: a sequence's keys are divided evenly, whatever its length, so that short sequences beside long
+// ones leave no workgroup idle and the long ones none behind.
+IPTQ_DEV int32_t wave_keys_of(const CacheAttentionArgs &A, int32_t length)
+{
+    return kTile * (int32_t)div_by((uint32_t)length + A.by_span.d - 1, A.by_span);
+}
+IPTQ_DEV int32_t length_of(const CacheAttentionArgs &A, uint32_t seq)
+{
+    return min(max(A.lengths[seq], 0), A.max_pages << A.C.page_log);
+}
 
 typedef i32x4 __attribute__((aligned(1))) i32x4_any;
 
@@ -97,16 +107,17 @@ struct CacheAttention {
     int32_t page_of_block;                                // lane l: page of the wavefront's block l, or -1
     i32x4 q[G];
 
-    IPTQ_DEV CacheAttention(const CacheAttentionArgs &a, uint32_t kvh_, uint32_t seq_, uint32_t e0, int32_t from_, int32_t keys, int8_t *stage_)
-        : A(a), lane(threadIdx.x & 63), col(lane & 15), p(lane >> 4), stage(stage_), kvh(kvh_), seq(seq_), from(from_)
+    // first: the wavefront's number among those that the sequence's keys are divided over
+    IPTQ_DEV CacheAttention(const CacheAttentionArgs &a, uint32_t kvh_, uint32_t seq_, uint32_t e0, int32_t first, int8_t *stage_)
+        : A(a), lane(threadIdx.x & 63), col(lane & 15), p(lane >> 4), stage(stage_), kvh(kvh_), seq(seq_)
     {
-        // the table's entries do not wait for the length: they are looked up inside the table and judged afterwards
-        const int32_t capacity = A.max_pages << A.C.page_log, key = from + 16 * lane;
-        const int32_t page = key < capacity ? (A.pages + (int64_t)seq * A.max_pages)[key >> A.C.page_log] : -1;
-        length = min(max(A.lengths[seq], 0), capacity);
+        length = length_of(A, seq);
+        const int32_t keys = wave_keys_of(A, length);
+        from = first * keys;
         to = min(length, from + keys);
+        const int32_t key = from + 16 * lane;
+        page_of_block = page_of_key(A.pages + (int64_t)seq * A.max_pages, A.C.page_log, A.C.n_pages, key, to);
         e = min(e0 + (col & (QUERIES - 1)), (uint32_t)A.columns - 1);     // columns past the last repeat it
-        page_of_block = key < to && page >= 0 && page < A.C.n_pages ? page : -1;
     }
     IPTQ_DEV uint32_t token() const { return div_by(e, A.by_group); }
     IPTQ_DEV int64_t q_row(uint32_t token) const { return (int64_t)seq * A.q_tokens + token; }
@@ -234,7 +245,10 @@ struct CacheAttention {
             w[i] = weights_of_pair<VARIANT>(t, A.P);
             *sum = __builtin_amdgcn_udot2(__builtin_bit_cast(u16x2_t, w[i]), (u16x2_t){1, 1}, *sum, false);
         }
+        // u = (w a + 64) >> 7 is the upper part of t = 2 w a + 128, from bit 8 on; with 128 more of u in it, its upper byte
+        // is the upper half of u and its lower byte the lower half with the sign turned
         i32x4 hi[G], lo[G];
+        const uint32_t select = HALVES == 2 && col >= 8 ? 0x06040200u : 0x07050301u, turn = HALVES == 2 && col < 8 ? 0u : 0x80808080u;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -242,16 +256,17 @@ struct CacheAttention {
                 uint32_t u[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint32_t ww = w[2 * i + j];
-                    const uint32_t a = __umul24(ww & 0xffff, (uint32_t)byte_of(v.steps, (4 * i + 2 * j) * G + g)) + 64;
-                    const uint32_t b = __umul24(ww >> 16, (uint32_t)byte_of(v.steps, (4 * i + 2 * j + 1) * G + g)) + 64;
-                    u[j] = a >> 7 | b >> 7 << 16;
+                    const u16x2_t w2 = __builtin_bit_cast(u16x2_t, w[2 * i + j]) << (unsigned short)1;
+                    const int at0 = (4 * i + 2 * j) * G + g, at1 = at0 + G;           // the steps' bytes
+                    const uint32_t a = __builtin_amdgcn_perm(0u, v.steps[at0 >> 4][at0 >> 2 & 3], 0x0c0c0c00u | (at0 & 3));
+                    const uint32_t b = __builtin_amdgcn_perm(0u, v.steps[at1 >> 4][at1 >> 2 & 3], 0x0c000c0cu | (at1 & 3) << 16);
+                    const uint32_t ta = __builtin_amdgcn_udot2(w2, __builtin_bit_cast(u16x2_t, a), 128u + 32768u, false);
+                    const uint32_t tb = __builtin_amdgcn_udot2(w2, __builtin_bit_cast(u16x2_t, b), 128u + 32768u, false);
+                    u[j] = __builtin_amdgcn_perm(tb, ta, 0x06050201u);
                 }
-                uint32_t h, l;
-                split_weights(u[0], u[1], &h, &l);
-                hi[g][i] = (int32_t)h;
-                lo[g][i] = (int32_t)l;
-                if (HALVES == 2) hi[g][i] = col < 8 ? hi[g][i] : lo[g][i];
+                hi[g][i] = (int32_t)__builtin_amdgcn_perm(u[1], u[0], select);
+                if (HALVES == 2) hi[g][i] = (int32_t)((uint32_t)hi[g][i] ^ turn);
+                else lo[g][i] = (int32_t)(__builtin_amdgcn_perm(u[1], u[0], 0x06040200u) ^ turn);
             }
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
@@ -293,13 +308,14 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
     int32_t *lds_top = lds + 16 * c, *lds_acc = lds + 32 * ct + c * T::ACC;
     uint32_t *lds_sum = reinterpret_cast<uint32_t *>(lds + 16 * ct + 16 * c);
     const int e_wg = (int)chunk * T::QUERIES * ct;                         // the workgroup's first query
-    T t(A, kvh, seq, (uint32_t)(e_wg + T::QUERIES * c), (int32_t)split * A.split_keys + key_wave * A.wave_keys, A.wave_keys,
+    T t(A, kvh, seq, (uint32_t)(e_wg + T::QUERIES * c), (int32_t)split * A.key_waves + key_wave,
         lds_bytes + wave * T::STAGE);
     const int lane = t.lane, col = t.col, p = t.p;
-    if (PHASES != 3 && (int32_t)split * A.split_keys >= t.length) return; // no key in this split
+    const int32_t split_keys = wave_keys_of(A, t.length) * A.key_waves;
+    if (PHASES != 3 && (int32_t)split * split_keys >= t.length) return;   // no key in this split
     t.load_queries();
     const int64_t pair = (int64_t)seq * A.C.kv_heads + kvh;
-    const int32_t tiles = (A.split_keys * A.splits) / kTile;               // of a sequence's share of the workspace
+    const int32_t tiles = A.tiles;
     const int columns = PHASES == 3 ? T::QUERIES * ct : A.columns;
     int16_t *deltas = PHASES == 3 ? reinterpret_cast<int16_t *>(lds + (32 + T::ACC) * ct) : A.deltas + pair * tiles * 4 * columns * 16;
     int32_t *refs = PHASES == 3 ? lds + (32 + T::ACC) * ct + tiles * 4 * columns * 8 : A.refs + pair * tiles * columns;
@@ -341,9 +357,8 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
         __syncthreads();
     }
     if (PHASES == 2) {                                    // the largest score of all splits that have keys
-        const int32_t live = div_by((uint32_t)(t.length + A.split_keys - 1), A.by_split_keys);
         const int log = ct == 2 ? 5 : 4;
-        for (int i = threadIdx.x & (16 * ct - 1), s = threadIdx.x >> log; s < live; s += blockDim.x >> log) {
+        for (int i = threadIdx.x & (16 * ct - 1), s = threadIdx.x >> log; s < A.splits && s * split_keys < t.length; s += blockDim.x >> log) {
             const int j = i & 15, x = e_wg + (i >> 4) * T::QUERIES + (j & (T::QUERIES - 1));
             if (x < columns) atomicMax(lds + i, A.tops[(pair * A.splits + s) * columns + x]);
         }

@@ -13,12 +13,11 @@ __global__ __launch_bounds__(256) void attention_cache_i4_join_kernel(const Cach
     const uint32_t pair = div_by(blockIdx.x, A.by_columns), column = blockIdx.x - pair * A.by_columns.d;
     const uint32_t seq = div_by(pair, A.by_kv_heads), kvh = pair - seq * A.by_kv_heads.d;
     const int dim = A.C.dim, unit = threadIdx.x & 15, part = threadIdx.x >> 4, wave = threadIdx.x >> 6;
-    const int32_t length = min(max(A.lengths[seq], 0), A.max_pages << A.C.page_log);
-    const int32_t live = (int32_t)div_by((uint32_t)(length + A.split_keys - 1), A.by_split_keys);
+    const int32_t length = length_of(A, seq), split_keys = wave_keys_of(A, length) * A.key_waves;
     int64_t v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     uint32_t s = 0;
     if (8 * unit < dim)
-        for (int32_t i = part; i < live; i += 16) {
+        for (int32_t i = part; i < A.splits && i * split_keys < length; i += 16) {
             const int64_t at = ((int64_t)pair * A.splits + i) * A.columns + column;
             const i32x4 *o = reinterpret_cast<const i32x4 *>(A.partial + at * dim + 8 * unit);
             const i32x4 a = o[0], b = o[1];
@@ -49,8 +48,7 @@ __global__ __launch_bounds__(256) void attention_cache_i4_join_kernel(const Cach
 struct CachePlan {
     int halves, ct, chunks;           // weights' halves side by side; column tiles of a workgroup; workgroups over the columns
     bool whole;                       // one workgroup has all keys
-    int key_waves;                    // of a workgroup
-    int32_t wave_keys, split_keys, splits;
+    int key_waves, splits, tiles;
     size_t lds;
     int64_t pairs, deltas, refs, tops, partial, sums;      // workspace bytes
 };
@@ -66,27 +64,26 @@ static CachePlan plan_of(const CacheAttentionCall &c)
     const int queries = 16 / p.halves * p.ct;
     p.chunks = (columns + queries - 1) / queries;
     p.pairs = (int64_t)c.n_seq * c.C.kv_heads;
-    const int64_t keys = std::max<int64_t>(up_to((int64_t)c.max_pages * c.C.page_tokens, kTile), kTile);
+    const int64_t keys = (int64_t)c.max_pages * c.C.page_tokens;           // at most
+    p.tiles = (int)((keys + kTile - 1) / kTile);
     p.whole = keys <= 1024;
-    p.key_waves = 4;
-    if (p.whole) {
-        p.wave_keys = keys <= 256 ? kTile : (int32_t)up_to(keys, 256) / 4;
-    } else {
-        // workgroups enough for the chip, but no more than the partial sums of each are worth
-        int64_t split = 256;
-        while (split < 4096 && (split < 64 * queries || keys * p.pairs * p.chunks / split > 4096)) split *= 2;
-        p.wave_keys = (int32_t)split / 4;
+    p.key_waves = p.whole || p.ct == 1 ? 4 : 2;
+    p.splits = 1;
+    if (!p.whole) {
+        // workgroups enough for the chip, a wavefront with 64 to 1024 keys; with many columns fewer, as each split
+        // writes and reads a sum per column and channel
+        const int64_t most = (keys + kTile * p.key_waves - 1) / (kTile * p.key_waves), least = (keys + 1024 * p.key_waves - 1) / (1024 * p.key_waves);
+        const int64_t wanted = (columns > 8 ? 1024 : 2048) / (p.pairs * p.chunks);
+        p.splits = (int)std::min<int64_t>(std::max(std::max<int64_t>(wanted, least), (int64_t)1), std::min<int64_t>(most, 128));
     }
-    p.split_keys = p.wave_keys * p.key_waves;
-    p.splits = (int32_t)((keys + p.split_keys - 1) / p.split_keys);
     const size_t blocks = c.C.dim / 32, stage = std::max(blocks * 4 * 288, (size_t)kTile * c.C.dim / 2 + 256);       // CacheAttention::STAGE
-    p.lds = (size_t)p.key_waves * p.ct * stage + (size_t)p.ct * (32 + c.C.dim / 32 * 512) * 4 + (p.whole ? (size_t)p.split_keys / kTile * queries * (4 * 32 + 4) : 0);
-    const int64_t rows = p.whole ? 0 : p.pairs * p.splits * columns, tiles = p.split_keys / kTile;
-    p.deltas = rows * p.split_keys * 2;
-    p.refs = up_to(rows * tiles * 4, 16);
-    p.tops = up_to(rows * 4, 16);
-    p.partial = rows * c.C.dim * 4;
-    p.sums = up_to(rows * 4, 16);
+    p.lds = (size_t)p.key_waves * p.ct * stage + (size_t)p.ct * (32 + c.C.dim / 32 * 512) * 4 + (p.whole ? (size_t)p.tiles * queries * (4 * 32 + 4) : 0);
+    const int64_t rows = p.whole ? 0 : p.pairs * columns;
+    p.deltas = rows * p.tiles * kTile * 2;
+    p.refs = up_to(rows * p.tiles * 4, 16);
+    p.tops = up_to(rows * p.splits * 4, 16);
+    p.partial = rows * p.splits * c.C.dim * 4;
+    p.sums = up_to(rows * p.splits * 4, 16);
     return p;
 }
 
@@ -118,10 +115,11 @@ hipError_t attention_cache_i4_dispatch(const CacheAttentionCall &c, hipStream_t 
     a.by_kv_heads = div_of((uint32_t)c.C.kv_heads);
     a.by_chunks = div_of((uint32_t)p.chunks);
     a.by_splits = div_of((uint32_t)p.splits);
-    a.by_split_keys = div_of((uint32_t)p.split_keys);
+    a.by_span = div_of((uint32_t)(kTile * p.key_waves * p.splits));
     a.by_columns = div_of((uint32_t)a.columns);
     a.column_tiles = p.ct;
-    a.split_keys = p.split_keys; a.splits = p.splits; a.wave_keys = p.wave_keys;
+    a.key_waves = p.key_waves;
+    a.splits = p.splits; a.tiles = p.tiles;
     char *w = static_cast<char *>(c.work);
     a.deltas = reinterpret_cast<int16_t *>(w); w += p.deltas;
     a.partial = reinterpret_cast<int32_t *>(w); w += p.partial;
