@@ -25,7 +25,6 @@ struct AttentionArgs {
     int64_t q_stride, k_stride, v_stride, out_stride;
     const int32_t *q_offsets, *k_offsets;
     int32_t q_tokens, k_tokens, q_len, k_len, max_q;      // q_len, k_len: of every sequence where there are no offsets
-    int32_t kv_heads, group;
     DivDev by_kv_heads, by_group, by_seq;                 // workgroup number -> kv head, head of its group, sequence, tile
     uint32_t tiles;
     AttentionDev P;
@@ -64,98 +63,157 @@ IPTQ_DEV void weights_of_scores(const i32x16 &x, const AttentionDev &P, i32x4 *h
     }
 }
 
+// What a workgroup works on: a sequence's queries [q0, q0 + nq) and keys [k0, k0 + nk) among the tokens, the first query of its tile.
+struct AttentionTile {
+    uint32_t head, kvh;
+    int32_t q0, nq, k0, nk, diag, first;
+};
+// false: nothing to do
+IPTQ_DEV bool attention_tile(const AttentionArgs &A, uint32_t wg, int queries, AttentionTile *t)
+{
+    const uint32_t r1 = div_by(wg, A.by_kv_heads);
+    t->kvh = wg - r1 * A.by_kv_heads.d;
+    const uint32_t r2 = div_by(r1, A.by_group);
+    t->head = t->kvh * A.by_group.d + (r1 - r2 * A.by_group.d);
+    const uint32_t r3 = div_by(r2, A.by_seq), seq = r2 - r3 * A.by_seq.d;
+    t->first = (int32_t)(A.tiles - 1 - r3) * queries;     // the longest rows first
+    if (A.q_offsets) {
+        clamped_range(A.q_offsets[seq], A.q_offsets[seq + 1], A.q_tokens, &t->q0, &t->nq);
+        clamped_range(A.k_offsets[seq], A.k_offsets[seq + 1], A.k_tokens, &t->k0, &t->nk);
+        if (t->nk > IPTQ_KEYS_MAX) return false;          // not served: its rows are left as they were
+    } else {
+        t->nq = A.q_len; t->nk = A.k_len;
+        t->q0 = (int32_t)seq * t->nq; t->k0 = (int32_t)seq * t->nk;
+    }
+    t->diag = t->nk - t->nq;                              // causal: query i sees keys 0 .. i + diag
+    t->nq = min(t->nq, A.max_q);
+    return t->first < t->nq;
+}
+
+// Where the sums of shifted scores start so that they come out stabilised: x' - max x' ==
+// (x + rounding - (max x' << shift)) >> shift.
+IPTQ_DEV int32_t score_start(int32_t top, int shift)
+{
+    const int32_t rounding = shift > 0 ? 1 << (shift - 1) : 0;
+    return top == kI32Min ? 0 : rounding - (((top + rounding) >> shift) << shift);
+}
+
+// Rows of V in LDS, bytes: eight of them, 32 bytes of each, meet all banks once.
+template <int D> struct ValueRow { static constexpr int bytes = D == 128 ? 160 : D == 64 ? 96 : D; };
+
+typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
+// Left operand of the second product, 32 channels x 32 keys, out of rows of keys: the transposing read gives a lane
+// eight keys' bytes of one channel.  src: the lane's address for the block's first eight keys.
+template <int ROW>
+IPTQ_DEV i32x4 values_of_block(const int8_t *src)
+{
+    typedef __attribute__((address_space(3))) i32x2 *Lds;
+    const i32x2 a = __builtin_amdgcn_ds_read_tr8_b64_v2i32((Lds)(uintptr_t)(src));
+    const i32x2 b = __builtin_amdgcn_ds_read_tr8_b64_v2i32((Lds)(uintptr_t)(src + 8 * ROW));
+    return (i32x4){a.x, a.y, b.x, b.y};
+}
+
+// 16 outputs of a 32-channel block: floor(2^54 / sum) times the sums, 46 bits down, requantized.
+IPTQ_DEV void store_block(int8_t *out, uint64_t f, const i32x16 &hi, const i32x16 &lo, int half, const DyadicDev &post)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t bytes = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t acc = (int64_t)hi[4 * i + j] * 256 + lo[4 * i + j];
+            bytes |= (uint32_t)(mean_byte(f, acc, 46, post) & 255) << (8 * j);
+        }
+        *reinterpret_cast<i32_a1 *>(out + 8 * i + 4 * half) = (int32_t)bytes;
+    }
+}
+
 template <int D, int VARIANT>
-__global__ __launch_bounds__(64 * kWaves) void attention_i8_kernel(const AttentionArgs A)
+__global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const AttentionArgs A)
 {
     constexpr int STEPS = D / 32;                     // 32-channel steps of the first product, blocks of the second
-    constexpr int KROW = D + 16, VROW = kKeys + 16;   // LDS rows in bytes, padded
-    __shared__ __attribute__((aligned(16))) int8_t lds_k[kKeys * KROW];
-    __shared__ __attribute__((aligned(16))) int8_t lds_v[D * VROW];
+    constexpr int KROW = D + 16, VROW = ValueRow<D>::bytes;
+    constexpr int CHUNKS = kKeys * D / 16, LOADS = (CHUNKS + 64 * kWaves - 1) / (64 * kWaves);
+    __shared__ __attribute__((aligned(16))) int8_t lds_k[2][kKeys * KROW];
+    __shared__ __attribute__((aligned(16))) int8_t lds_v[2][kKeys * VROW];
 
-    const uint32_t wg = blockIdx.x;
-    const uint32_t r1 = div_by(wg, A.by_kv_heads), kvh = wg - r1 * (uint32_t)A.kv_heads;
-    const uint32_t r2 = div_by(r1, A.by_group), head = kvh * (uint32_t)A.group + (r1 - r2 * (uint32_t)A.group);
-    const uint32_t r3 = div_by(r2, A.by_seq), seq = r2 - r3 * A.by_seq.d;
-    const int32_t tile0 = (int32_t)(A.tiles - 1 - r3) * kQueries;       // the longest rows first
-
-    int32_t q0, k0, nq, nk;
-    if (A.q_offsets) {
-        clamped_range(A.q_offsets[seq], A.q_offsets[seq + 1], A.q_tokens, &q0, &nq);
-        clamped_range(A.k_offsets[seq], A.k_offsets[seq + 1], A.k_tokens, &k0, &nk);
-        if (nk > IPTQ_KEYS_MAX) return;               // not served: its rows are left as they were
-    } else {
-        nq = A.q_len; nk = A.k_len;
-        q0 = (int32_t)seq * nq; k0 = (int32_t)seq * nk;
-    }
-    const int32_t diag = nk - nq;                     // causal: query i sees keys 0 .. i + diag
-    nq = min(nq, A.max_q);
-    if (tile0 >= nq) return;
-
+    AttentionTile T;
+    if (!attention_tile(A, blockIdx.x, kQueries, &T)) return;
+    const int32_t nq = T.nq, nk = T.nk;
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int32_t first = tile0 + 32 * wave;          // the wavefront's first query
+    const int32_t first = T.first + 32 * wave;        // the wavefront's first query
     const int32_t row = first + col;
-    const int32_t limit = A.P.causal ? min(max(row + diag + 1, 0), nk) : nk;
+    const int32_t limit = A.P.causal ? min(max(row + T.diag + 1, 0), nk) : nk;
     // keys that any / every row of the wavefront sees, and that any row of the workgroup sees
-    const int32_t wave_most = first >= nq ? 0 : A.P.causal ? min(max(min(first + 32, nq) + diag, 0), nk) : nk;
-    const int32_t wave_least = A.P.causal ? min(max(first + diag + 1, 0), nk) : nk;
-    const int32_t most = A.P.causal ? min(max(min(tile0 + kQueries, nq) + diag, 0), nk) : nk;
+    const int32_t wave_most = first >= nq ? 0 : A.P.causal ? min(max(min(first + 32, nq) + T.diag, 0), nk) : nk;
+    const int32_t wave_least = A.P.causal ? min(max(first + T.diag + 1, 0), nk) : nk;
+    const int32_t most = A.P.causal ? min(max(min(T.first + kQueries, nq) + T.diag, 0), nk) : nk;
 
     i32x4 qf[STEPS];
     {
-        const int8_t *p = A.q + (int64_t)(q0 + min(row, nq - 1)) * A.q_stride + head * D + 16 * half;
+        const int8_t *p = A.q + (int64_t)(T.q0 + min(row, nq - 1)) * A.q_stride + T.head * D + 16 * half;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const i32x4_a1 *>(p + 32 * s);
     }
-    const int8_t *kp = A.k + (int64_t)k0 * A.k_stride + kvh * D, *vp = A.v + (int64_t)k0 * A.v_stride + kvh * D;
+    const int8_t *kp = A.k + (int64_t)T.k0 * A.k_stride + T.kvh * D, *vp = A.v + (int64_t)T.k0 * A.v_stride + T.kvh * D;
 
-    auto stage_k = [&](int32_t at) {
-        for (int u = threadIdx.x; u < kKeys * D / 16; u += 64 * kWaves) {
-            const int key = u / (D / 16), c = u - key * (D / 16);
-            const i32x4 t = *reinterpret_cast<const i32x4_a1 *>(kp + (int64_t)min(at + key, nk - 1) * A.k_stride + 16 * c);
-            *reinterpret_cast<i32x4 *>(lds_k + key_row(key) * KROW + 16 * c) = t;
-        }
+    // the thread's share of a tile: 16-byte chunks; keys past the last repeat it
+    int chunk_key[LOADS], chunk_at[LOADS];
+    bool chunk_mine[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int u = threadIdx.x + 64 * kWaves * i;
+        chunk_mine[i] = CHUNKS % (64 * kWaves) == 0 || u < CHUNKS;
+        chunk_key[i] = u / (D / 16);
+        chunk_at[i] = 16 * (u - chunk_key[i] * (D / 16));
+    }
+    auto load = [&](const int8_t *base, int64_t stride, int32_t at, i32x4 (&t)[LOADS]) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            if (chunk_mine[i]) t[i] = *reinterpret_cast<const i32x4_a1 *>(base + (int64_t)min(at + chunk_key[i], nk - 1) * stride + chunk_at[i]);
     };
-    auto stage_v = [&](int32_t at) {                  // transposed: four keys' bytes of one channel side by side
-        for (int u = threadIdx.x; u < kKeys * D / 16; u += 64 * kWaves) {
-            const int g = u / (D / 4), c = u - g * (D / 4);
-            uint32_t t[4];
+    auto stage_k = [&](int buffer, const i32x4 (&t)[LOADS]) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                t[j] = *reinterpret_cast<const i32_a1 *>(vp + (int64_t)min(at + 4 * g + j, nk - 1) * A.v_stride + 4 * c);
-            const uint32_t a = __builtin_amdgcn_perm(t[1], t[0], 0x05010400u), b = __builtin_amdgcn_perm(t[1], t[0], 0x07030602u);
-            const uint32_t e = __builtin_amdgcn_perm(t[3], t[2], 0x05010400u), f = __builtin_amdgcn_perm(t[3], t[2], 0x07030602u);
-            uint32_t *o = reinterpret_cast<uint32_t *>(lds_v + 4 * c * VROW + 4 * g);
-            o[0] = __builtin_amdgcn_perm(e, a, 0x05040100u);
-            o[VROW / 4] = __builtin_amdgcn_perm(e, a, 0x07060302u);
-            o[2 * VROW / 4] = __builtin_amdgcn_perm(f, b, 0x05040100u);
-            o[3 * VROW / 4] = __builtin_amdgcn_perm(f, b, 0x07060302u);
-        }
+        for (int i = 0; i < LOADS; ++i)
+            if (chunk_mine[i]) *reinterpret_cast<i32x4 *>(lds_k[buffer] + key_row(chunk_key[i]) * KROW + chunk_at[i]) = t[i];
     };
-    // transposed scores of keys [32 b, 32 b + 32) of the staged tile; init: where the sums start
-    auto scores = [&](int b, int32_t init) {
-        i32x16 x;
+    auto stage_v = [&](int buffer, const i32x4 (&t)[LOADS]) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = init;
+        for (int i = 0; i < LOADS; ++i)
+            if (chunk_mine[i]) *reinterpret_cast<i32x4 *>(lds_v[buffer] + chunk_key[i] * VROW + chunk_at[i]) = t[i];
+    };
+    // transposed scores of keys [32 b, 32 b + 32) of a staged tile
+    auto scores = [&](int buffer, int b, const i32x16 &start) {
+        const int8_t *src = lds_k[buffer] + (32 * b + col) * KROW + 16 * half;
+        i32x16 x = start;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const i32x4 kf = *reinterpret_cast<const i32x4 *>(lds_k + (32 * b + col) * KROW + 32 * s + 16 * half);
-            x = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf, qf[s], x, 0, 0, 0);
-        }
+        for (int s = 0; s < STEPS; ++s)
+            x = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const i32x4 *>(src + 32 * s), qf[s], x, 0, 0, 0);
         return x;
     };
 
     // first run over the keys: the row's maximum
+    i32x4 kr[LOADS], vr[LOADS];
+    i32x16 start;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) start[i] = 0;
     int32_t top = kI32Min;
-    for (int32_t at = 0; at < most; at += kKeys) {
-        __syncthreads();
-        stage_k(at);
-        __syncthreads();
+    if (most > 0) {
+        load(kp, A.k_stride, 0, kr);
+        stage_k(0, kr);
+    }
+    __syncthreads();
+    int buffer = 0;
+    for (int32_t at = 0; at < most; at += kKeys, buffer ^= 1) {
+        const bool more = at + kKeys < most;
+        load(kp, A.k_stride, more ? at + kKeys : 0, kr);      // the next tile, behind the last one the first again
+        if (!more) load(vp, A.v_stride, 0, vr);
 #pragma unroll
         for (int b = 0; b < kKeys / 32; ++b) {
             const int32_t k1 = at + 32 * b;
             if (k1 >= wave_most) break;
-            const i32x16 x = scores(b, 0);
+            const i32x16 x = scores(buffer, b, start);
             if (k1 + 32 <= wave_least) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = max(top, x[i]);
@@ -164,11 +222,16 @@ __global__ __launch_bounds__(64 * kWaves) void attention_i8_kernel(const Attenti
                 for (int i = 0; i < 16; ++i) top = k1 + 16 * half + i < limit ? max(top, x[i]) : top;
             }
         }
+        stage_k(buffer ^ 1, kr);
+        if (!more) stage_v(buffer ^ 1, vr);
+        __syncthreads();
     }
     top = max(top, __shfl_xor(top, 32));
-    // x' - max x' == (x + rounding - (max x' << shift)) >> shift: the sums start at what lies behind x
-    const int32_t rounding = A.P.shift > 0 ? 1 << (A.P.shift - 1) : 0;
-    const int32_t init = top == kI32Min ? 0 : rounding - (((top + rounding) >> A.P.shift) << A.P.shift);
+    {
+        const int32_t v = score_start(top, A.P.shift);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) start[i] = v;
+    }
 
     // second run: weights and weighted values
     i32x16 acc_hi[STEPS], acc_lo[STEPS];
@@ -177,16 +240,19 @@ __global__ __launch_bounds__(64 * kWaves) void attention_i8_kernel(const Attenti
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc_hi[s][i] = acc_lo[s][i] = 0;
     uint32_t sum = 0;
-    for (int32_t at = 0; at < most; at += kKeys) {
-        __syncthreads();
-        stage_k(at);
-        stage_v(at);
-        __syncthreads();
+    // the lane's part of a transposing read: key (lane % 16) / 2 of eight, channels 16 (lane / 16 % 2) + 8 (lane % 2) of 32
+    const int v_lane = (16 * half + (lane >> 1 & 7)) * VROW + 16 * (lane >> 4 & 1) + 8 * (lane & 1);
+    for (int32_t at = 0; at < most; at += kKeys, buffer ^= 1) {
+        const bool more = at + kKeys < most;
+        if (more) {
+            load(kp, A.k_stride, at + kKeys, kr);
+            load(vp, A.v_stride, at + kKeys, vr);
+        }
 #pragma unroll
         for (int b = 0; b < kKeys / 32; ++b) {
             const int32_t k1 = at + 32 * b;
             if (k1 >= wave_most) break;
-            i32x16 x = scores(b, init);
+            i32x16 x = scores(buffer, b, start);
             if (k1 + 32 > wave_least) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[i] = k1 + 16 * half + i < limit ? x[i] : kI32Min;
@@ -195,28 +261,23 @@ __global__ __launch_bounds__(64 * kWaves) void attention_i8_kernel(const Attenti
             weights_of_scores<VARIANT>(x, A.P, &hi, &lo, &sum);
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
-                const i32x4 vf = *reinterpret_cast<const i32x4 *>(lds_v + (32 * s + col) * VROW + 32 * b + 16 * half);
+                const i32x4 vf = values_of_block<VROW>(lds_v[buffer] + 32 * b * VROW + v_lane + 32 * s);
                 acc_hi[s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vf, hi, acc_hi[s], 0, 0, 0);
                 acc_lo[s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vf, lo, acc_lo[s], 0, 0, 0);
             }
         }
+        if (more) {
+            stage_k(buffer ^ 1, kr);
+            stage_v(buffer ^ 1, vr);
+        }
+        __syncthreads();
     }
     sum += (uint32_t)__shfl_xor((int32_t)sum, 32);
     if (row >= nq) return;
     const uint64_t f = floor_div_u64((uint64_t)1 << 54, sum);
-    int8_t *out = A.out + (int64_t)(q0 + row) * A.out_stride + head * D;
+    int8_t *out = A.out + (int64_t)(T.q0 + row) * A.out_stride + T.head * D;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t bytes = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t acc = (int64_t)acc_hi[s][4 * i + j] * 256 + acc_lo[s][4 * i + j];
-                bytes |= (uint32_t)(mean_byte(f, acc, 46, A.P.post) & 255) << (8 * j);
-            }
-            *reinterpret_cast<i32_a1 *>(out + 32 * s + 8 * i + 4 * half) = (int32_t)bytes;
-        }
+    for (int s = 0; s < STEPS; ++s) store_block(out + 32 * s, f, acc_hi[s], acc_lo[s], half, A.P.post);
 }
 
 hipError_t attention_i8_launch_32(const AttentionArgs &a, uint32_t grid, hipStream_t stream);

@@ -12,9 +12,8 @@ hipError_t attention_i8_dispatch(const AttentionCall &c, hipStream_t stream)
     a.q_tokens = (int32_t)c.q_tokens; a.k_tokens = (int32_t)c.k_tokens;
     a.q_len = (int32_t)(c.q_tokens / c.n_seq); a.k_len = (int32_t)(c.k_tokens / c.n_seq);
     a.max_q = c.max_q;
-    a.kv_heads = c.kv_heads; a.group = c.heads / c.kv_heads;
     a.by_kv_heads = div_of((uint32_t)c.kv_heads);
-    a.by_group = div_of((uint32_t)a.group);
+    a.by_group = div_of((uint32_t)(c.heads / c.kv_heads));
     a.by_seq = div_of((uint32_t)c.n_seq);
     a.tiles = ((uint32_t)c.max_q + kQueries - 1) / kQueries;
     a.P = c.P;
