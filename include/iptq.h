@@ -436,7 +436,7 @@ int iptq_attention_cache_i4(const int8_t *d_q, int64_t q_stride, const iptq_cach
  * d_residual_out: NULL or rows * cols int32 (r; may be d_residual itself, in place).  No other overlap of an output.
  * |in_m| < 2^15; 0 <= in_s <= 62; 0 <= eps <= 2^46 (in units of the stream's squares); 1 <= cols <= IPTQ_NORM_COLS_MAX.
  */
-#define IPTQ_NORM_COLS_MAX 32768
+#define IPTQ_NORM_COLS_MAX 16384
 typedef struct {
     int32_t in_m, in_s;
     int64_t eps;

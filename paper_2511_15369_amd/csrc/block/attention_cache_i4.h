@@ -242,9 +242,13 @@ struct CacheAttention {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const i16x2 t = __builtin_elementwise_max(__builtin_elementwise_add_sat(__builtin_bit_cast(i16x2, d[i]), offs), least);
-            w[i] = weights_of_pair<VARIANT>(t, A.P);
-            *sum = __builtin_amdgcn_udot2(__builtin_bit_cast(u16x2_t, w[i]), (u16x2_t){1, 1}, *sum, false);
+            w[i] = __builtin_bit_cast(uint32_t, t);
         }
+        uint32_t (&w0)[4] = *reinterpret_cast<uint32_t (*)[4]>(w), (&w1)[4] = *reinterpret_cast<uint32_t (*)[4]>(w + 4);
+        weights_of_pairs<VARIANT, 4>(w0, A.P);
+        weights_of_pairs<VARIANT, 4>(w1, A.P);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) *sum = __builtin_amdgcn_udot2(__builtin_bit_cast(u16x2_t, w[i]), (u16x2_t){1, 1}, *sum, false);
         // u = (w a + 64) >> 7 is the upper part of t = 2 w a + 128, from bit 8 on; with 128 more of u in it, its upper byte
         // is the upper half of u and its lower byte the lower half with the sign turned
         i32x4 hi[G], lo[G];

@@ -46,20 +46,26 @@ IPTQ_DEV void weights_of_scores(const i32x16 &x, const AttentionDev &P, i32x4 *h
 {
     const i16x2 least = {(short)-P.d_clamp, (short)-P.d_clamp};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t w[2];
+    for (int g = 0; g < 2; ++g) {                         // eight scores at a time
+        uint32_t w[4];
+        int32_t t[8];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int32_t a = x[4 * i + 2 * j] >> P.shift, b = x[4 * i + 2 * j + 1] >> P.shift;
-            i16x2 d = __builtin_bit_cast(i16x2, __builtin_amdgcn_cvt_pk_i16(a, b));
-            d = __builtin_elementwise_max(d, least);
-            w[j] = weights_of_pair<VARIANT>(d, P);
-            *sum = __builtin_amdgcn_udot2(__builtin_bit_cast(u16x2_t, w[j]), (u16x2_t){1, 1}, *sum, false);
+        for (int i = 0; i < 8; ++i) t[i] = x[8 * g + i] >> P.shift;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2, __builtin_amdgcn_cvt_pk_i16(t[2 * i], t[2 * i + 1])), least));
+        weights_of_pairs<VARIANT, 4>(w, P);
+        uint32_t part[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[i & 1] = __builtin_amdgcn_udot2(__builtin_bit_cast(u16x2_t, w[i]), (u16x2_t){1, 1}, i < 2 ? (i ? 0u : *sum) : part[i & 1], false);
+        *sum = part[0] + part[1];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t h, l;
+            split_weights(w[2 * i], w[2 * i + 1], &h, &l);
+            (*hi)[2 * g + i] = (int32_t)h;
+            (*lo)[2 * g + i] = (int32_t)l;
         }
-        uint32_t h, l;
-        split_weights(w[0], w[1], &h, &l);
-        (*hi)[i] = (int32_t)h;
-        (*lo)[i] = (int32_t)l;
     }
 }
 
@@ -209,6 +215,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const Atte
         const bool more = at + kKeys < most;
         load(kp, A.k_stride, more ? at + kKeys : 0, kr);      // the next tile, behind the last one the first again
         if (!more) load(vp, A.v_stride, 0, vr);
+        if (at + kKeys <= wave_least) {
+            const i32x16 x = scores(buffer, 0, start), y = scores(buffer, 1, start);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = max(max(top, x[i]), y[i]);
+        } else
 #pragma unroll
         for (int b = 0; b < kKeys / 32; ++b) {
             const int32_t k1 = at + 32 * b;
@@ -248,23 +259,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const Atte
             load(kp, A.k_stride, at + kKeys, kr);
             load(vp, A.v_stride, at + kKeys, vr);
         }
-#pragma unroll
-        for (int b = 0; b < kKeys / 32; ++b) {
-            const int32_t k1 = at + 32 * b;
-            if (k1 >= wave_most) break;
-            i32x16 x = scores(buffer, b, start);
-            if (k1 + 32 > wave_least) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = k1 + 16 * half + i < limit ? x[i] : kI32Min;
-            }
-            i32x4 hi, lo;
-            weights_of_scores<VARIANT>(x, A.P, &hi, &lo, &sum);
+        auto values = [&](int b, const i32x4 &hi, const i32x4 &lo) {
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
                 const i32x4 vf = values_of_block<VROW>(lds_v[buffer] + 32 * b * VROW + v_lane + 32 * s);
                 acc_hi[s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vf, hi, acc_hi[s], 0, 0, 0);
                 acc_lo[s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vf, lo, acc_lo[s], 0, 0, 0);
             }
+        };
+        if (at < wave_most) {
+            i32x16 x = scores(buffer, 0, start), y = scores(buffer, 1, start);
+            if (at + kKeys > wave_least) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    x[i] = at + 16 * half + i < limit ? x[i] : kI32Min;
+                    y[i] = at + 32 + 16 * half + i < limit ? y[i] : kI32Min;
+                }
+            }
+            i32x4 hi, lo;
+            weights_of_scores<VARIANT>(x, A.P, &hi, &lo, &sum);
+            values(0, hi, lo);
+            weights_of_scores<VARIANT>(y, A.P, &hi, &lo, &sum);
+            values(1, hi, lo);
         }
         if (more) {
             stage_k(buffer ^ 1, kr);

@@ -123,15 +123,22 @@ IPTQ_HD uint64_t floor_div_u64(uint64_t num, uint32_t den)
     return q;
 }
 
-// floor(sqrt(v)) for 2^60 <= v < 2^62, one bit of the root after another from the top.
+// floor(sqrt(v)) for 2^60 <= v < 2^62: Newton's iteration for 1 / sqrt(a), a = v / 2^62 in [1/4, 1), in 32 bits, one step of the
+// remainder in 64, and the last unit by trial.  (Bit by bit it was the longest part of a short call's chain.)
 IPTQ_HD uint32_t root_u62(uint64_t v)
 {
-    uint32_t root = 1u << 30;
-    for (uint32_t bit = 1u << 29; bit != 0; bit >>= 1) {
-        const uint32_t t = root | bit;
-        root = (uint64_t)t * t <= v ? t : root;
+    const uint32_t a = (uint32_t)(v >> 30);               // Q32
+    uint32_t y = 2469606196u - mulhi_u32(a, 1471026135u); // 2.3 - 1.37 a in Q30: within a seventh
+    for (int i = 0; i < 5; ++i) {                         // y (3 - a y^2) / 2
+        const uint32_t t = mulhi_u32(a, mulhi_u32(y, y)); // Q28, about 1
+        y = mulhi_u32(y, 805306368u - t) << 3;
     }
-    return root;
+    uint32_t r = mulhi_u32(a, y) << 1;                    // Q32 Q30 -> Q30, wanted in Q31
+    const int64_t left = (int64_t)(v - (uint64_t)r * r);
+    r += (uint32_t)(((left >> 8) * (int64_t)y) >> 54);    // 1 / (2 sqrt(v)) = y / 2^32
+    while ((uint64_t)r * r > v) --r;
+    while ((uint64_t)(r + 1) * (r + 1) <= v) ++r;
+    return r;
 }
 
 // ---- what the device reads of tables and offsets, kept inside the tensors -----------------------------------
@@ -151,29 +158,67 @@ IPTQ_HD int32_t page_of_key(const int32_t *table, int page_log, int32_t n_pages,
 }
 
 // ---- weights ------------------------------------------------------------------------------------
-// The bit-shifting exponentials of two scores side by side in 16-bit halves: `d` is the stabilised score of
-// either, clamped at -D, the result (base << N) >> q below 2^15 - 128 (Eq. 7-10, 13-14; the second degree).
-template <int VARIANT>
-IPTQ_DEV uint32_t weights_of_pair(i16x2 d, const AttentionDev &P)
+// The bit-shifting exponentials of 2 N scores in 16-bit halves: `d` are stabilised scores, clamped at -D, the results
+// (base << N) >> q below 2^15 - 128 (Eq. 7-10, 13-14; the second degree).  Every packed step is N independent
+// instructions side by side: a pair alone is one chain, each of whose links waits for the one before.
+// The compiler would undo that to save registers: only products, scalar and memory instructions may pass the ends of a step.
+IPTQ_DEV void end_of_step() { __builtin_amdgcn_sched_barrier(0x9c); }
+template <int N> struct Pairs { uint32_t v[N]; };
+template <int VARIANT, int N>
+IPTQ_DEV void weights_of_pairs(uint32_t (&d)[N], const AttentionDev &P)
 {
-    const i16x2 m = (d + (d >> (short)1)) - (d >> (short)4);           // Qp of Eq. 7, in (-2^15, 0]
-    const uint32_t mw = __builtin_bit_cast(uint32_t, m);
+    typedef short S __attribute__((ext_vector_type(2 * N)));
+    typedef unsigned short U __attribute__((ext_vector_type(2 * N)));
+    typedef Pairs<N> W;
+    const S x = __builtin_bit_cast(S, *reinterpret_cast<W *>(d));
+    const S half = x >> (short)1;
+    end_of_step();
+    const S more = x + half;
+    end_of_step();
+    const S sixteenth = x >> (short)4;
+    end_of_step();
+    const S m = more - sixteenth;                                      // Qp of Eq. 7, in (-2^15, 0]
+    end_of_step();
+    const W mw = __builtin_bit_cast(W, m);
     // Eq. 8: (-m) div i0 is the top byte of (-m) ceil(2^24 / i0), both factors negated
-    const uint32_t a = (uint32_t)__mul24((int32_t)(int16_t)mw, P.div8);
-    const uint32_t b = (uint32_t)__mul24((int32_t)mw >> 16, P.div8);
-    const u16x2_t q = __builtin_bit_cast(u16x2_t, (uint32_t)__builtin_amdgcn_perm(b, a, 0x0c070c03u));
-    const i16x2 nr = (i16x2)(q * (unsigned short)P.i0 + (u16x2_t)m);   // -r in (-i0, 0]
-    i16x2 fr = nr >> (short)1;                                         // Eq. 10
-    if (VARIANT >= 1) fr = fr + (nr >> (short)3) + (nr >> (short)4);   // Eq. 13
+    W qw;
+    uint32_t a[N], b[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        a[i] = (uint32_t)__mul24((int32_t)(int16_t)mw.v[i], P.div8);
+        b[i] = (uint32_t)__mul24((int32_t)mw.v[i] >> 16, P.div8);
+    }
+    end_of_step();
+#pragma unroll
+    for (int i = 0; i < N; ++i) qw.v[i] = __builtin_amdgcn_perm(b[i], a[i], 0x0c070c03u);
+    end_of_step();
+    const U q = __builtin_bit_cast(U, qw);
+    const S nr = (S)(q * (unsigned short)P.i0 + (U)m);                 // -r in (-i0, 0]
+    end_of_step();
+    S fr = nr >> (short)1;                                             // Eq. 10
+    if (VARIANT >= 1) {                                                // Eq. 13
+        end_of_step();
+        const S eighth = nr >> (short)3;
+        end_of_step();
+        fr = fr + eighth;
+        const S last = nr >> (short)4;
+        end_of_step();
+        fr = fr + last;
+    }
     if (VARIANT == 2) {                                                // Eq. 11, second degree
-        const int32_t y0 = fr[0], y1 = fr[1];
-        i16x2 t;
-        t[0] = (short)(mulhi_u32((uint32_t)__mul24(y0, y0), P.d2_magic) >> P.d2_sh);
-        t[1] = (short)(mulhi_u32((uint32_t)__mul24(y1, y1), P.d2_magic) >> P.d2_sh);
+        S t;
+#pragma unroll
+        for (int i = 0; i < 2 * N; ++i) {
+            const int32_t y = fr[i];
+            t[i] = (short)(mulhi_u32((uint32_t)__mul24(y, y), P.d2_magic) >> P.d2_sh);
+        }
         fr = fr + t;
     }
-    const u16x2_t base = (u16x2_t)fr * (unsigned short)(1u << P.n_shift) + (unsigned short)P.i0n;
-    return __builtin_bit_cast(uint32_t, (u16x2_t)(base >> q));         // q <= 15
+    end_of_step();
+    const U base = (U)fr * (unsigned short)(1u << P.n_shift) + (unsigned short)P.i0n;
+    end_of_step();
+    *reinterpret_cast<W *>(d) = __builtin_bit_cast(W, (U)(base >> q)); // q <= 15
+    end_of_step();
 }
 
 // Weights as the two 8-bit factors of a signed matrix product: w = 256 hi + lo with lo in [-128, 127], so

@@ -1,7 +1,48 @@
 // Root-mean-square norm with the residual's addition, and requantization by row scales.
+//
+// Both are bound by HBM: 13 bytes per value of the norm (product, residual, its new value, code), 5 of the requantization.
+// A row stays in the registers of the wavefronts that hold it, so every byte crosses once.  Rows are read in chunks of four
+// values at their natural alignment; where four does not divide a row its last chunk ends with it and starts
+// earlier, and the values it shares with the chunk before count once.
+#include <algorithm>
+
 #include "block.h"
 
 namespace iptq {
+
+constexpr int32_t kResidualMost = (1 << 23) - 1;
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef i16x4 __attribute__((aligned(2))) i16x4_a2;
+
+// rshr_round(x m, s) for |x| < 2^31, |m| < 2^15.  FAST: s >= 16, one multiplication and a shift of its upper half (mul
+// and rnd moved up to where the result's lowest bit is the upper half's), and the result fits 32 bits.
+struct ShiftDev {
+    int32_t m, s;
+    int32_t mul, sh;
+    int64_t rnd;
+};
+static ShiftDev shift_of(int32_t m, int32_t s)
+{
+    return {m, s, s >= 16 ? (int32_t)((uint32_t)m << (s <= 32 ? 32 - s : 0)) : 0, s > 32 ? s - 32 : 0, s >= 16 ? pre_rnd_of(s) : s > 0 ? (int64_t)1 << (s - 1) : 0};
+}
+IPTQ_DEV int32_t shifted_fast(int32_t x, const ShiftDev &S) { return (int32_t)(((int64_t)x * S.mul + S.rnd) >> 32) >> S.sh; }
+IPTQ_DEV int64_t shifted(int32_t x, const ShiftDev &S) { return ((int64_t)x * S.m + S.rnd) >> S.s; }
+
+// clamp(rshr_round(x m, s) + zp, qmin, qmax)
+template <bool FAST>
+IPTQ_DEV int32_t code_of(int32_t x, const ShiftDev &S, const DyadicDev &P)
+{
+    if (FAST) return clamp_i32(shifted_fast(x, S) + P.zp, P.qmin, P.qmax);      // (|x m| < 2^46: 2^30 at most, and zp 2^24)
+    int64_t v = shifted(x, S) + P.zp;
+    v = v < P.qmin ? P.qmin : v > P.qmax ? P.qmax : v;
+    return (int32_t)v;
+}
+IPTQ_DEV uint32_t four_bytes(const int32_t (&c)[4])
+{
+    const uint32_t a = __builtin_amdgcn_perm((uint32_t)c[1], (uint32_t)c[0], 0x0c0c0400u);
+    return __builtin_amdgcn_perm((uint32_t)c[3], (uint32_t)c[2], 0x04000c0cu) | a;
+}
 
 struct RmsnormArgs {
     const int32_t *x, *residual;
@@ -9,100 +50,276 @@ struct RmsnormArgs {
     const int16_t *gain;
     int8_t *out;
     int32_t *row_scales;
-    int32_t cols;
-    int32_t in_m, in_s;
+    int32_t rows, cols;
     int64_t eps_sum;
     uint32_t root_cols;
-    DyadicDev post;
+    ShiftDev in, post;
+    DyadicDev p;
 };
 
-constexpr int32_t kResidualMost = (1 << 23) - 1;
-
-IPTQ_DEV int64_t rounded_shift(int64_t v, int s) { return s > 0 ? (v + ((int64_t)1 << (s - 1))) >> s : v; }
-
-// A row in LDS: sum of squares, root and factor, then the codes.
-__global__ __launch_bounds__(256) void rmsnorm_i32_kernel(const RmsnormArgs A)
+// The factor of a row from its sum of squares, and the shift that goes with it: z = rshr_round(r c, 41 - t).
+IPTQ_DEV uint32_t row_factor(uint64_t total, uint32_t root_cols, int *t)
 {
-    extern __shared__ int32_t row[];
-    __shared__ uint64_t parts[4];
-    __shared__ uint32_t tops[4];
-    const int64_t at = (int64_t)blockIdx.x * A.cols;
+    *t = 0;
+    if (total == 0) return 0;
+    const uint32_t top = (uint32_t)(total >> 32);
+    const int bits = top != 0 ? 64 - clz_u32(top) : 32 - clz_u32((uint32_t)total);
+    *t = (62 - bits) >> 1;
+    const uint32_t inverse = (uint32_t)floor_div_u64((uint64_t)1 << 61, root_u62(total << (2 * *t)));
+    return (uint32_t)(((uint64_t)root_cols * inverse) >> 24);
+}
+IPTQ_DEV uint64_t at_most_62_bits(uint64_t v) { return v >= ((uint64_t)1 << 62) ? ((uint64_t)1 << 62) - 1 : v; }
+
+// WAVES wavefronts per row (1: four rows a workgroup, no barrier), CHUNKS chunks of four values per lane.
+// FAST: both steps' shifts are 16 and more.
+template <int WAVES, int CHUNKS, bool FAST>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rmsnorm_i32_kernel(const RmsnormArgs A)
+{
+    constexpr int T = 64 * WAVES;
+    __shared__ uint32_t parts[2][WAVES];
+    __shared__ uint32_t tops[WAVES];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int tid = WAVES == 1 ? lane : threadIdx.x;
+    const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+    if (WAVES == 1 && row >= A.rows) return;
+    const int64_t at = row * A.cols;
+    const int cols = A.cols;
+
+    int start[CHUNKS];
+    bool mine[CHUNKS];
+    i32x4 r[CHUNKS], add[CHUNKS];
+    i16x4 g[CHUNKS];
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+        const int c = 4 * (tid + T * i);
+        mine[i] = c < cols;
+        start[i] = min(c, cols - 4);                      // (lanes past the row read its last chunk)
+        r[i] = A.x ? load_i32x4(A.x + at + start[i]) : (i32x4){0, 0, 0, 0};
+        add[i] = A.residual ? load_i32x4(A.residual + at + start[i]) : (i32x4){0, 0, 0, 0};
+        g[i] = *reinterpret_cast<const i16x4_a2 *>(A.gain + start[i]);
+    }
     uint64_t ss = 0;
-    for (int i = threadIdx.x; i < A.cols; i += 256) {
-        int64_t v = A.x ? rounded_shift((int64_t)A.x[at + i] * A.in_m, A.in_s) : 0;
-        if (A.residual) v += A.residual[at + i];
-        v = v > kResidualMost ? kResidualMost : v < -kResidualMost ? -kResidualMost : v;
-        row[i] = (int32_t)v;
-        if (A.residual_out) A.residual_out[at + i] = (int32_t)v;
-        ss += (uint64_t)(v * v);
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+        const int skip = mine[i] ? 4 * (tid + T * i) - start[i] : 4;      // values that the chunk before has counted
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            int32_t v;
+            if (FAST) {
+                v = sat_add_i32(A.x ? shifted_fast(r[i][e], A.in) : 0, add[i][e]);
+                v = clamp_i32(v, -kResidualMost, kResidualMost);
+            } else {
+                int64_t w = (A.x ? shifted(r[i][e], A.in) : 0) + add[i][e];
+                v = (int32_t)(w > kResidualMost ? kResidualMost : w < -kResidualMost ? -kResidualMost : w);
+            }
+            r[i][e] = v;
+            const int32_t counted = e >= skip ? v : 0;
+            ss += (uint64_t)((int64_t)counted * counted);
+        }
     }
-    for (int d = 1; d < 64; d <<= 1) ss += __shfl_xor((unsigned long long)ss, d);
-    if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = ss;
-    __syncthreads();
-    uint64_t total = parts[0] + parts[1] + parts[2] + parts[3] + (uint64_t)A.eps_sum;
-    total = total >= ((uint64_t)1 << 62) ? ((uint64_t)1 << 62) - 1 : total;
-    uint32_t c = 0;
-    int t = 0;
-    if (total != 0) {
-        const uint32_t top = (uint32_t)(total >> 32);
-        const int bits = top != 0 ? 64 - clz_u32(top) : 32 - clz_u32((uint32_t)total);
-        t = (62 - bits) >> 1;
-        const uint32_t inv = (uint32_t)floor_div_u64((uint64_t)1 << 61, root_u62(total << (2 * t)));
-        c = (uint32_t)(((uint64_t)A.root_cols * inv) >> 24);
+    // two parts of 26 bits and what is above, either a sum of 64 lanes in 32 bits
+    uint32_t lo = wave_sum_u32((uint32_t)ss & 0x3ffffffu), hi = wave_sum_u32((uint32_t)(ss >> 26));
+    uint64_t total = (uint64_t)lo + ((uint64_t)hi << 26);
+    if (WAVES > 1) {
+        if (lane == 0) { parts[0][wave] = (uint32_t)total; parts[1][wave] = (uint32_t)(total >> 32); }
+        __syncthreads();
+        total = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) total += (uint64_t)parts[0][i] | (uint64_t)parts[1][i] << 32;
     }
+    // (behind the loads of the whole row: the stream may be updated in place)
+    if (A.residual_out) {
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+            if (mine[i]) *reinterpret_cast<i32x4_a4 *>(A.residual_out + at + start[i]) = r[i];
+        }
+    }
+    int t;
+    const uint32_t c = row_factor(at_most_62_bits(total + (uint64_t)A.eps_sum), A.root_cols, &t);
+    const int64_t half = (int64_t)1 << (40 - t);
+    const int shift = 41 - t;
     uint32_t most = 0;
-    for (int i = threadIdx.x; i < A.cols; i += 256) {
-        const int32_t z = (int32_t)(((int64_t)row[i] * c + ((int64_t)1 << (40 - t))) >> (41 - t));
-        const int32_t y = (int32_t)(((int64_t)z * A.gain[i] + 32) >> 6);
-        row[i] = y;
-        most = max(most, (uint32_t)(y < 0 ? -y : y));
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int32_t z = (int32_t)(((int64_t)r[i][e] * (int32_t)c + half) >> shift);
+            const int32_t y = (int32_t)(((int64_t)z * g[i][e] + 32) >> 6);
+            r[i][e] = y;
+            most = max(most, (uint32_t)max(y, -y));
+        }
     }
     if (A.row_scales) {
-        for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
-        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = most;
-        __syncthreads();
-        most = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
-        if (threadIdx.x == 0) A.row_scales[blockIdx.x] = (int32_t)most;
-        const int64_t f = (int64_t)floor_div_u64((uint64_t)127 << 40, most);
-        for (int i = threadIdx.x; i < A.cols; i += 256) A.out[at + i] = (int8_t)((row[i] * f + ((int64_t)1 << 39)) >> 40);
+        most = (uint32_t)wave_max_i32((int32_t)most);
+        if (WAVES > 1) {
+            if (lane == 0) tops[wave] = most;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) most = max(most, tops[i]);
+        }
+        if (tid == 0) A.row_scales[row] = (int32_t)most;
+        // y f / 2^40 with f = floor(127 2^40 / most): y's and f's upper parts carry it, but the rounding wants all of it
+        const uint64_t f = floor_div_u64((uint64_t)127 << 40, most);
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+            int32_t code[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) code[e] = (int32_t)(((int64_t)r[i][e] * (int64_t)f + ((int64_t)1 << 39)) >> 40);
+            if (mine[i]) *reinterpret_cast<u32_a1 *>(A.out + at + start[i]) = four_bytes(code);
+        }
     } else {
-        for (int i = threadIdx.x; i < A.cols; i += 256)
-            A.out[at + i] = (int8_t)requant_dev<false>(row[i], A.post.m, A.post.s, A.post.zp, A.post.qmin, A.post.qmax);
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+            int32_t code[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) code[e] = code_of<FAST>(r[i][e], A.post, A.p);
+            if (mine[i]) *reinterpret_cast<u32_a1 *>(A.out + at + start[i]) = four_bytes(code);
+        }
     }
+}
+
+// Rows of one to three values: one per thread.
+__global__ __launch_bounds__(256) void rmsnorm_narrow_kernel(const RmsnormArgs A)
+{
+    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (row >= A.rows) return;
+    int32_t r[3] = {0, 0, 0};
+    uint64_t ss = (uint64_t)A.eps_sum;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        if (i >= A.cols) break;
+        int64_t w = A.x ? shifted(A.x[row * A.cols + i], A.in) : 0;
+        if (A.residual) w += A.residual[row * A.cols + i];
+        r[i] = (int32_t)(w > kResidualMost ? kResidualMost : w < -kResidualMost ? -kResidualMost : w);
+        ss += (uint64_t)((int64_t)r[i] * r[i]);
+        if (A.residual_out) A.residual_out[row * A.cols + i] = r[i];
+    }
+    int t;
+    const uint32_t c = row_factor(at_most_62_bits(ss), A.root_cols, &t);
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        if (i >= A.cols) break;
+        const int32_t z = (int32_t)(((int64_t)r[i] * (int32_t)c + ((int64_t)1 << (40 - t))) >> (41 - t));
+        r[i] = (int32_t)(((int64_t)z * A.gain[i] + 32) >> 6);
+        most = max(most, (uint32_t)max(r[i], -r[i]));
+    }
+    if (A.row_scales) A.row_scales[row] = (int32_t)most;
+    const uint64_t f = A.row_scales ? floor_div_u64((uint64_t)127 << 40, most) : 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        if (i >= A.cols) break;
+        A.out[row * A.cols + i] = (int8_t)(A.row_scales ? (int32_t)(((int64_t)r[i] * (int64_t)f + ((int64_t)1 << 39)) >> 40) : code_of<false>(r[i], A.post, A.p));
+    }
+}
+
+template <int WAVES, int CHUNKS>
+static void rmsnorm_launch(const RmsnormArgs &a, bool fast, hipStream_t stream)
+{
+    const uint32_t grid = WAVES == 1 ? ((uint32_t)a.rows + 3) / 4 : (uint32_t)a.rows;
+    launch_kernel(fast ? rmsnorm_i32_kernel<WAVES, CHUNKS, true> : rmsnorm_i32_kernel<WAVES, CHUNKS, false>, dim3(grid),
+                  dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, stream, a);
 }
 
 hipError_t rmsnorm_i32_dispatch(const RmsnormCall &c, hipStream_t stream)
 {
     RmsnormArgs a;
     a.x = c.x; a.residual = c.residual; a.residual_out = c.residual_out; a.gain = c.gain; a.out = c.out; a.row_scales = c.row_scales;
-    a.cols = c.cols; a.in_m = c.in_m; a.in_s = c.in_s; a.eps_sum = c.eps_sum; a.root_cols = c.root_cols; a.post = c.post;
-    launch_kernel(rmsnorm_i32_kernel, dim3((uint32_t)c.rows), dim3(256), (size_t)c.cols * 4, stream, a);
+    a.rows = (int32_t)c.rows; a.cols = c.cols; a.eps_sum = c.eps_sum; a.root_cols = c.root_cols;
+    a.in = shift_of(c.in_m, c.in_s);
+    a.post = shift_of(c.post.m, c.post.s);
+    a.p = c.post;
+    const bool fast = c.in_s >= 16 && (c.post.s >= 16 || c.row_scales);
+    if (c.cols < 4) {
+        a.in.rnd = c.in_s > 0 ? (int64_t)1 << (c.in_s - 1) : 0;            // (the general form of both steps)
+        a.post.rnd = c.post.s > 0 ? (int64_t)1 << (c.post.s - 1) : 0;
+        launch_kernel(rmsnorm_narrow_kernel, dim3(((uint32_t)c.rows + 255) / 256), dim3(256), 0, stream, a);
+        return take_launch_status();
+    }
+    if (!fast) {
+        a.in.rnd = c.in_s > 0 ? (int64_t)1 << (c.in_s - 1) : 0;
+        a.post.rnd = c.post.s > 0 ? (int64_t)1 << (c.post.s - 1) : 0;
+    }
+    const int chunks = (c.cols + 3) / 4;
+    // Wavefronts per row: one up to 1024 values; beyond, four with up to eight chunks a lane while there are rows enough to fill the
+    // chip, else as many as give a lane one or two.
+    const bool few = c.rows < 1024;
+    if (chunks <= 64) rmsnorm_launch<1, 1>(a, fast, stream);
+    else if (chunks <= 128 && !few) rmsnorm_launch<1, 2>(a, fast, stream);
+    else if (chunks <= 256 && !few) rmsnorm_launch<1, 4>(a, fast, stream);
+    else if (chunks <= 256) rmsnorm_launch<4, 1>(a, fast, stream);
+    else if (chunks <= 512 && !few) rmsnorm_launch<4, 2>(a, fast, stream);
+    else if (chunks <= 768 && !few) rmsnorm_launch<4, 3>(a, fast, stream);
+    else if (chunks <= 1024 && !few) rmsnorm_launch<4, 4>(a, fast, stream);
+    else if (chunks <= 1280 && !few) rmsnorm_launch<4, 5>(a, fast, stream);
+    else if (chunks <= 1536 && !few) rmsnorm_launch<4, 6>(a, fast, stream);
+    else if (chunks <= 2048 && !few) rmsnorm_launch<4, 8>(a, fast, stream);
+    else if (chunks <= 1024) rmsnorm_launch<16, 1>(a, fast, stream);
+    else if (chunks <= 2048) rmsnorm_launch<16, 2>(a, fast, stream);
+    else rmsnorm_launch<16, 4>(a, fast, stream);
     return take_launch_status();
 }
 
+// ---- requantization by row scales ---------------------------------------------------------------
 struct RequantRowsArgs {
     const int32_t *in, *row_scales;
     uint8_t *out;
+    int64_t rnd;                      // of row_shift
     int32_t cols, row_shift;
+    uint32_t chunks, wgs;             // of the launch
+    DivDev by_row;                    // chunks of a row
+    ShiftDev S;
     DyadicDev P;
 };
 
+IPTQ_DEV int32_t saturated(int64_t v)
+{
+    const int32_t lo = (int32_t)v, hi = (int32_t)(v >> 32);
+    return hi == lo >> 31 ? lo : hi >> 31 ^ 0x7fffffff;
+}
+
+// WIDTH 4: chunks of four values; 1: rows of fewer, one value each.
+template <int WIDTH, bool FAST>
 __global__ __launch_bounds__(256) void requant_rows_kernel(const RequantRowsArgs A)
 {
-    const int64_t at = (int64_t)blockIdx.x * A.cols;
-    const int64_t scale = A.row_scales[blockIdx.x];
-    for (int i = threadIdx.x; i < A.cols; i += 256) {
-        int64_t v = rounded_shift(A.in[at + i] * scale, A.row_shift);
-        v = v > INT32_MAX ? INT32_MAX : v < INT32_MIN ? INT32_MIN : v;
-        A.out[at + i] = (uint8_t)requant_dev<false>((int32_t)v, A.P.m, A.P.s, A.P.zp, A.P.qmin, A.P.qmax);
+    const uint32_t step = 256 * A.wgs;
+    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < A.chunks; i += step) {
+        const uint32_t row = div_by(i, A.by_row);
+        const int c = WIDTH * (int)(i - row * A.by_row.d), start = WIDTH == 4 ? min(c, A.cols - 4) : c;
+        const int64_t at = (int64_t)row * A.cols + start;
+        const int32_t scale = A.row_scales[row];
+        if (WIDTH == 4) {
+            const i32x4 x = stream_load_i32x4(A.in + at);
+            int32_t code[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) code[e] = code_of<FAST>(saturated(((int64_t)x[e] * scale + A.rnd) >> A.row_shift), A.S, A.P);
+            stream_store_bytes4(four_bytes(code), A.out + at);
+        } else {
+            A.out[at] = (uint8_t)code_of<FAST>(saturated(((int64_t)A.in[at] * scale + A.rnd) >> A.row_shift), A.S, A.P);
+        }
     }
 }
 
 hipError_t requant_rows_dispatch(const int32_t *in, const int32_t *row_scales, int32_t row_shift, void *out, int64_t rows,
                                  int32_t cols, const DyadicDev &P, hipStream_t stream)
 {
-    const RequantRowsArgs a = {in, row_scales, static_cast<uint8_t *>(out), cols, row_shift, P};
-    launch_kernel(requant_rows_kernel, dim3((uint32_t)rows), dim3(256), 0, stream, a);
+    RequantRowsArgs a;
+    a.rnd = row_shift > 0 ? (int64_t)1 << (row_shift - 1) : 0;
+    a.cols = cols; a.row_shift = row_shift;
+    a.S = shift_of(P.m, P.s);
+    a.P = P;
+    const int width = cols < 4 ? 1 : 4;
+    const int64_t per_row = (cols + width - 1) / width, most_rows = (((int64_t)1 << 30) / per_row);
+    a.by_row = div_of((uint32_t)per_row);
+    for (int64_t r = 0; r < rows; r += most_rows) {       // (chunks are counted in 32 bits)
+        const int64_t n = rows - r < most_rows ? rows - r : most_rows;
+        a.in = in + r * cols; a.row_scales = row_scales + r; a.out = static_cast<uint8_t *>(out) + r * cols;
+        a.chunks = (uint32_t)(n * per_row);
+        a.wgs = std::min((a.chunks + 255) / 256, 16384u);
+        auto kernel = width == 4 ? (P.s >= 16 ? requant_rows_kernel<4, true> : requant_rows_kernel<4, false>)
+                                 : (P.s >= 16 ? requant_rows_kernel<1, true> : requant_rows_kernel<1, false>);
+        launch_kernel(kernel, dim3(a.wgs), dim3(256), 0, stream, a);
+    }
     return take_launch_status();
 }
 

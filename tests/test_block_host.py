@@ -139,7 +139,7 @@ def norm_params(**k):
 
 
 @pytest.mark.parametrize("code,change", [
-    (0, {}), (NULL, dict(p=None)), (SHAPE, dict(rows=-1)), (SHAPE, dict(rows=1 << 31)), (SHAPE, dict(cols=0)), (SHAPE, dict(cols=32769)),
+    (0, {}), (NULL, dict(p=None)), (SHAPE, dict(rows=-1)), (SHAPE, dict(rows=1 << 31)), (SHAPE, dict(cols=0)), (SHAPE, dict(cols=16385)),
     (PARAM, dict(p=norm_params(m=32768))), (PARAM, dict(p=norm_params(m=-32768))), (PARAM, dict(p=norm_params(s=63))),
     (PARAM, dict(p=norm_params(eps=-1))), (PARAM, dict(p=norm_params(eps=2 ** 46 + 1))), (PARAM, dict(p=norm_params(post=ip.Dyadic(1, 0, 0, 0, 128)))),
     (NULL, dict(rows=1, x=None, r=None, ro=None)), (NULL, dict(rows=1, g=None)), (NULL, dict(rows=1, out=None)), (ALIGN, dict(rows=1, x=BASE + 2)),

@@ -359,8 +359,7 @@ def _norm(rng, rows, cols, scales, x=True, residual=True, keep=True, in_place=Fa
         assert np.array_equal(s.cpu().numpy()[:rows], want[2]) and int(s[rows]) == 77
 
 
-@pytest.mark.parametrize("cols", [1, 2, 3, 63, 64, 65, 255, 256, 257, 1000, 1023, 1024, 2047, 2048, 2052, 4096, 4100, 5120, 8191, 8192, 8193, 12288, 16384, 16385,
-                                  20001, 32767, 32768])
+@pytest.mark.parametrize("cols", [1, 2, 3, 63, 64, 65, 255, 256, 257, 1000, 1023, 1024, 2047, 2048, 2052, 4096, 4100, 5120, 8191, 8192, 8193, 12288, 12289, 16383, 16384])
 @pytest.mark.parametrize("scales", [False, True])
 def test_norm_lengths(cols, scales):
     rng = np.random.default_rng([cols, scales])
