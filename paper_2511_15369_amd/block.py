@@ -57,6 +57,22 @@ def _lib():
     return lib
 
 
+_native_of = None                 # the library that the native calls are bound to
+
+
+def _native():
+    """The native call module bound to these entry points, once the first call of the process has been made; or None."""
+    global _native_of
+    call = binding._fast
+    if call is not None and _native_of is not binding._lib:
+        lib = _lib()
+        call.bind_block(*[ctypes.cast(getattr(lib, "iptq_" + n), ctypes.c_void_p).value for n in
+                          ("attention_i8", "cache_store_i4", "attention_cache_i4", "rmsnorm_i32", "requant_rows")],
+                        AttentionParams, RmsnormParams, CacheI4, Dyadic)
+        _native_of = binding._lib
+    return call
+
+
 def _need(t, dtype, what, least=0):
     torch = binding.torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
@@ -93,6 +109,11 @@ def attention_prepare(s_score: float, s_v: float, s_out: float, zp_out: int, var
 def attention_i8(d_q, d_k, d_v, d_q_offsets, d_k_offsets, n_seq: int, max_q: int, d_out, p: AttentionParams):
     """d_q, d_out: int8 [q tokens, heads, head dimension]; d_k, d_v: [k tokens, kv heads, head dimension]; rows
     may lie apart.  Offsets: int32 [n_seq + 1] both, or None both (equal lengths)."""
+    call = _native()
+    if call is not None:
+        rc = call.attention_i8(d_q, d_k, d_v, d_q_offsets, d_k_offsets, n_seq, max_q, d_out, p)
+        if rc is not None:
+            return _check(rc, "iptq_attention_i8")
     lib = _lib()
     qt, heads, dim, qs = _rows(d_q, "d_q")
     kt, kv_heads, kd, ks = _rows(d_k, "d_k")
@@ -129,6 +150,11 @@ def cache_i4(d_k_codes, d_k_steps, d_v_codes, d_v_steps, head_dim: int) -> Cache
 
 def cache_store_i4(cache: CacheI4, d_k, d_v, d_slots, tokens: int):
     """d_k, d_v: int8 [tokens, kv heads, head dimension], rows may lie apart; d_slots: int32 [tokens]."""
+    call = _native()
+    if call is not None:
+        rc = call.cache_store_i4(cache, d_k, d_v, d_slots, tokens)
+        if rc is not None:
+            return _check(rc, "iptq_cache_store_i4")
     lib = _lib()
     kt, kh, kd, ks = _rows(d_k, "d_k")
     vt, vh, vd, vs = _rows(d_v, "d_v")
@@ -149,6 +175,11 @@ def attention_cache_i4_workspace(cache: CacheI4, n_seq: int, q_tokens: int, head
 def attention_cache_i4(d_q, cache: CacheI4, d_pages, d_lengths, n_seq: int, q_tokens: int, d_out, d_work, p: AttentionParams):
     """d_q, d_out: int8 [n_seq * q_tokens, heads, head dimension]; d_pages: int32 [n_seq, max_pages]; d_lengths: int32
     [n_seq]; d_work: uint8 of attention_cache_i4_workspace() bytes, or None."""
+    call = _native()
+    if call is not None:
+        rc = call.attention_cache_i4(d_q, cache, d_pages, d_lengths, n_seq, q_tokens, d_out, d_work, p)
+        if rc is not None:
+            return _check(rc, "iptq_attention_cache_i4")
     lib = _lib()
     qt, heads, dim, qs = _rows(d_q, "d_q")
     ot, oh, od, os_ = _rows(d_out, "d_out")
@@ -170,6 +201,11 @@ def attention_cache_i4(d_q, cache: CacheI4, d_pages, d_lengths, n_seq: int, q_to
 def rmsnorm_i32(d_x, d_residual, d_gain, d_residual_out, d_out, d_row_scales, rows: int, cols: int, p: RmsnormParams):
     """d_x, d_residual, d_residual_out: int32 [rows, cols] or None (d_residual_out may be d_residual); d_gain: int16 [cols];
     d_out: int8 [rows, cols]; d_row_scales: int32 [rows] or None (codes of one scale, by p.post)."""
+    call = _native()
+    if call is not None:
+        rc = call.rmsnorm_i32(d_x, d_residual, d_gain, d_residual_out, d_out, d_row_scales, rows, cols, p)
+        if rc is not None:
+            return _check(rc, "iptq_rmsnorm_i32")
     lib = _lib()
     torch = binding.torch
     n = rows * cols
@@ -185,6 +221,11 @@ def rmsnorm_i32(d_x, d_residual, d_gain, d_residual_out, d_out, d_row_scales, ro
 
 
 def requant_rows(d_in, d_row_scales, d_out, rows: int, cols: int, row_shift: int, out_is_signed: int, p: Dyadic):
+    call = _native()
+    if call is not None:
+        rc = call.requant_rows(d_in, d_row_scales, d_out, rows, cols, row_shift, out_is_signed, p)
+        if rc is not None:
+            return _check(rc, "iptq_requant_rows")
     lib = _lib()
     torch = binding.torch
     _need(d_in, torch.int32, "d_in", rows * cols)

@@ -9,6 +9,7 @@
 // raises what it always raised.  It calls the library through the addresses it was given.
 #include <Python.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -269,6 +270,157 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     Py_RETURN_NONE;
 }
 
+// ---- the block operators (block.py): bound apart, by bind_block()
+struct BoundBlock {
+    decltype(&iptq_attention_i8) attention_i8;
+    decltype(&iptq_cache_store_i4) cache_store_i4;
+    decltype(&iptq_attention_cache_i4) attention_cache_i4;
+    decltype(&iptq_rmsnorm_i32) rmsnorm_i32;
+    decltype(&iptq_requant_rows) requant_rows;
+    PyTypeObject *attention_params, *rmsnorm_params, *cache, *dyadic;
+} gb = {};
+
+// As tensor(), and on the current device; None: no pointer.
+bool local_tensor(PyObject *o, at::ScalarType type, int64_t least, void **p)
+{
+    return tensor(o, type, least, p) && THPVariable_Unpack(o).get_device() == c10::hip::current_device();
+}
+bool optional_tensor(PyObject *o, at::ScalarType type, int64_t least, void **p)
+{
+    *p = nullptr;
+    return o == Py_None || local_tensor(o, type, least, p);
+}
+
+// An int8 tensor [tokens, heads, head dimension] whose heads lie side by side in a token.
+struct Rows {
+    void *p;
+    int64_t tokens, heads, dim, stride;
+    bool take(PyObject *o)
+    {
+        if (!THPVariable_CheckExact(o)) return false;
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.scalar_type() != at::kChar || t.dim() != 3 || t.get_device() != c10::hip::current_device()) return false;
+        tokens = t.size(0); heads = t.size(1); dim = t.size(2);
+        if (tokens < 1 || heads < 1 || dim < 2 || heads > 65536 || dim > 65536) return false;
+        stride = tokens > 1 ? t.stride(0) : heads * dim;
+        if (t.stride(2) != 1 || (heads > 1 && t.stride(1) != dim) || stride < heads * dim) return false;
+        p = t.data_ptr();
+        return true;
+    }
+};
+
+PyObject *attention_i8(PyObject *const *a, Py_ssize_t n_args)
+{
+    Rows q, k, v, o;
+    void *qo, *ko;
+    int32_t n, max_q;
+    iptq_attention_params_t p;
+    if (n_args != 9 || gb.attention_i8 == nullptr || !integer(a[5], &n) || n < 0 || !integer(a[6], &max_q) || !q.take(a[0]) || !k.take(a[1]) ||
+        !v.take(a[2]) || !o.take(a[7]) || !structure(a[8], gb.attention_params, &p) ||
+        !optional_tensor(a[3], at::kInt, (int64_t)n + 1, &qo) || !optional_tensor(a[4], at::kInt, (int64_t)n + 1, &ko))
+        return nullptr;
+    if (k.tokens != v.tokens || k.heads != v.heads || q.dim != k.dim || q.dim != v.dim || q.tokens != o.tokens || q.heads != o.heads || q.dim != o.dim)
+        return nullptr;
+    return enqueue([&](void *s) {
+        return gb.attention_i8((const int8_t *)q.p, q.stride, (const int8_t *)k.p, k.stride, (const int8_t *)v.p, v.stride, (const int32_t *)qo,
+                               (const int32_t *)ko, n, max_q, q.tokens, k.tokens, (int32_t)q.heads, (int32_t)k.heads, (int32_t)q.dim,
+                               (int8_t *)o.p, o.stride, &p, s);
+    });
+}
+
+PyObject *cache_store_i4(PyObject *const *a, Py_ssize_t n_args)
+{
+    Rows k, v;
+    void *slots;
+    int64_t n;
+    iptq_cache_i4_t c;
+    if (n_args != 5 || gb.cache_store_i4 == nullptr || !structure(a[0], gb.cache, &c) || !k.take(a[1]) || !v.take(a[2]) || !integer(a[4], &n) ||
+        n < 0 || !local_tensor(a[3], at::kInt, n, &slots))
+        return nullptr;
+    if (k.tokens < n || v.tokens < n || k.heads != c.kv_heads || v.heads != c.kv_heads || k.dim != c.head_dim || v.dim != c.head_dim) return nullptr;
+    return enqueue([&](void *s) {
+        return gb.cache_store_i4(&c, (const int8_t *)k.p, k.stride, (const int8_t *)v.p, v.stride, (const int32_t *)slots, n, s);
+    });
+}
+
+PyObject *attention_cache_i4(PyObject *const *a, Py_ssize_t n_args)
+{
+    Rows q, o;
+    void *pages, *lengths, *work = nullptr;
+    int32_t n, t;
+    iptq_cache_i4_t c;
+    iptq_attention_params_t p;
+    if (n_args != 9 || gb.attention_cache_i4 == nullptr || !q.take(a[0]) || !structure(a[1], gb.cache, &c) || !integer(a[4], &n) || n < 0 ||
+        !integer(a[5], &t) || t < 0 || !o.take(a[6]) || !structure(a[8], gb.attention_params, &p) || !local_tensor(a[2], at::kInt, 0, &pages) ||
+        !local_tensor(a[3], at::kInt, n, &lengths) || !optional_tensor(a[7], at::kByte, 0, &work))
+        return nullptr;
+    const at::Tensor &table = THPVariable_Unpack(a[2]);
+    if (table.dim() != 2 || table.size(0) < n || table.size(1) > INT32_MAX || q.tokens != o.tokens || q.heads != o.heads || q.dim != o.dim ||
+        q.dim != c.head_dim || q.tokens < (int64_t)n * t)
+        return nullptr;
+    const int32_t max_pages = (int32_t)table.size(1);
+    const int64_t size = work ? THPVariable_Unpack(a[7]).numel() : 0;
+    return enqueue([&](void *s) {
+        return gb.attention_cache_i4((const int8_t *)q.p, q.stride, &c, (const int32_t *)pages, max_pages, (const int32_t *)lengths, n, t, (int32_t)q.heads,
+                                     (int8_t *)o.p, o.stride, work, size, &p, s);
+    });
+}
+
+PyObject *rmsnorm_i32(PyObject *const *a, Py_ssize_t n_args)
+{
+    void *x, *residual, *gain, *stream, *out, *scales;
+    int64_t rows;
+    int32_t cols;
+    iptq_rmsnorm_params_t p;
+    if (n_args != 9 || gb.rmsnorm_i32 == nullptr || !integer(a[6], &rows) || !integer(a[7], &cols) || !structure(a[8], gb.rmsnorm_params, &p)) return nullptr;
+    const int64_t n = elements(rows, cols);
+    if (n < 0 || !optional_tensor(a[0], at::kInt, n, &x) || !optional_tensor(a[1], at::kInt, n, &residual) || !local_tensor(a[2], at::kShort, cols, &gain) ||
+        !optional_tensor(a[3], at::kInt, n, &stream) || !local_tensor(a[4], at::kChar, n, &out) || !optional_tensor(a[5], at::kInt, rows, &scales))
+        return nullptr;
+    return enqueue([&](void *s) {
+        return gb.rmsnorm_i32((const int32_t *)x, (const int32_t *)residual, (const int16_t *)gain, (int32_t *)stream, (int8_t *)out, (int32_t *)scales, rows,
+                              cols, &p, s);
+    });
+}
+
+PyObject *requant_rows(PyObject *const *a, Py_ssize_t n_args)
+{
+    void *in, *scales, *out;
+    int64_t rows;
+    int32_t cols, shift, is_signed;
+    iptq_dyadic_t p;
+    if (n_args != 8 || gb.requant_rows == nullptr || !integer(a[3], &rows) || !integer(a[4], &cols) || !integer(a[5], &shift) || !integer(a[6], &is_signed) ||
+        !structure(a[7], gb.dyadic, &p))
+        return nullptr;
+    const int64_t n = elements(rows, cols);
+    if (n < 0 || !local_tensor(a[0], at::kInt, n, &in) || !local_tensor(a[1], at::kInt, rows, &scales) || !local_tensor(a[2], byte_type(is_signed), n, &out)) return nullptr;
+    return enqueue([&](void *s) { return gb.requant_rows((const int32_t *)in, (const int32_t *)scales, shift, out, rows, cols, is_signed, &p, s); });
+}
+
+// bind_block(addresses of the five entry points in the order of BoundBlock, AttentionParams, RmsnormParams, CacheI4, Dyadic)
+PyObject *bind_block(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    void *at[5];
+    bool right = n_args == 9;
+    for (int i = 0; right && i < 5; ++i) right = (at[i] = PyLong_AsVoidPtr(a[i])) != nullptr;
+    for (int i = 5; right && i < 9; ++i) right = PyType_Check(a[i]);
+    if (!right) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "bind_block takes five addresses and four classes");
+        return nullptr;
+    }
+    gb.attention_i8 = reinterpret_cast<decltype(gb.attention_i8)>(at[0]);
+    gb.cache_store_i4 = reinterpret_cast<decltype(gb.cache_store_i4)>(at[1]);
+    gb.attention_cache_i4 = reinterpret_cast<decltype(gb.attention_cache_i4)>(at[2]);
+    gb.rmsnorm_i32 = reinterpret_cast<decltype(gb.rmsnorm_i32)>(at[3]);
+    gb.requant_rows = reinterpret_cast<decltype(gb.requant_rows)>(at[4]);
+    PyTypeObject **types[4] = {&gb.attention_params, &gb.rmsnorm_params, &gb.cache, &gb.dyadic};
+    for (int i = 0; i < 4; ++i) {
+        Py_INCREF(a[5 + i]);                          // kept for the life of the process, as the module is
+        *types[i] = reinterpret_cast<PyTypeObject *>(a[5 + i]);
+    }
+    Py_RETURN_NONE;
+}
+
 #define IPTQ_METHOD(NAME, FN) {NAME, (PyCFunction)(void (*)(void))(FN), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     IPTQ_METHOD("bind", bind),
@@ -280,6 +432,12 @@ PyMethodDef methods[] = {
     IPTQ_METHOD("gelu_i32", guarded<gelu<false>>),
     IPTQ_METHOD("softmax_i32_layers", guarded<softmax_layers>),
     IPTQ_METHOD("gelu_i8_layers", guarded<gelu_layers>),
+    IPTQ_METHOD("bind_block", bind_block),
+    IPTQ_METHOD("attention_i8", guarded<attention_i8>),
+    IPTQ_METHOD("cache_store_i4", guarded<cache_store_i4>),
+    IPTQ_METHOD("attention_cache_i4", guarded<attention_cache_i4>),
+    IPTQ_METHOD("rmsnorm_i32", guarded<rmsnorm_i32>),
+    IPTQ_METHOD("requant_rows", guarded<requant_rows>),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
