@@ -37,7 +37,7 @@ struct CacheAttentionArgs {
     DivDev by_span, by_columns;                           // span: 64 keys of each wavefront that a sequence's keys are divided over
     int32_t column_tiles, key_waves;                      // of a workgroup: wavefronts side by side over the columns (1 or 2), over the keys
     int32_t splits, tiles;                                // workgroups over a sequence; tiles of the workspace a sequence
-    // between the phases: in LDS where one workgroup has all keys of a sequence, else here
+    // between the phases, where one workgroup does not have all keys of a sequence
     int16_t *deltas;                                      // [sequence, kv head][tile, p][2][column][8]
     int32_t *refs;                                        // [sequence, kv head][tile][column]
     int32_t *tops;                                        // [sequence, kv head][split][column]
@@ -74,7 +74,7 @@ IPTQ_DEV i32x4 in_nibble_order(i32x4 v)               // 16 channels of a query 
 }
 IPTQ_DEV int32_t byte_of(const u32x4 *v, int i) { return (int32_t)(v[i >> 4][i >> 2 & 3] >> (8 * (i & 3)) & 255u); }
 
-// PHASES 3: both, scores in LDS; 1: keys only; 2: values only.
+// PHASES 3: both, a tile a wavefront and its scores in registers; 1: keys only; 2: values only.
 // HALVES 2: up to eight queries share a kv head.  The second product's sixteen columns are then the upper halves of
 // eight queries' weights and the lower halves of the same: one product in place of two, and lanes that would have
 // been idle make the same weights as their neighbours.
@@ -299,8 +299,7 @@ IPTQ_DEV void store_means(int8_t *out, uint64_t f, const int64_t (&acc)[8], cons
 }
 
 // A workgroup's wavefronts: A.column_tiles of them side by side over the columns, the others over the keys.
-// LDS: a staging buffer per wavefront; per column tile [tops 16], [sums 16] and the sums [ACC]; (PHASES 3) deltas
-// [tiles * 4][2][queries][8] and refs [tiles][queries] with the queries of all column tiles.
+// LDS: a staging buffer per wavefront; per column tile [tops 16], [sums 16] and the sums [ACC].
 template <int D, int VARIANT, int HALVES, int PHASES>
 IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, uint32_t seq, uint32_t chunk, uint32_t split)
 {
@@ -320,18 +319,27 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
     t.load_queries();
     const int64_t pair = (int64_t)seq * A.C.kv_heads + kvh;
     const int32_t tiles = A.tiles;
-    const int columns = PHASES == 3 ? T::QUERIES * ct : A.columns;
-    int16_t *deltas = PHASES == 3 ? reinterpret_cast<int16_t *>(lds + (32 + T::ACC) * ct) : A.deltas + pair * tiles * 4 * columns * 16;
-    int32_t *refs = PHASES == 3 ? lds + (32 + T::ACC) * ct + tiles * 4 * columns * 8 : A.refs + pair * tiles * columns;
-    const int column = (PHASES == 3 ? 0 : e_wg) + T::QUERIES * c + (col & (T::QUERIES - 1));
+    const int columns = A.columns, column = e_wg + T::QUERIES * c + (col & (T::QUERIES - 1));
+    int16_t *deltas = A.deltas + pair * tiles * 4 * columns * 16;
+    int32_t *refs = A.refs + pair * tiles * columns;
     const bool mine = col < T::QUERIES && column < columns;                // the lane writes its column's scores
 
+    // (PHASES 3) the values are on their way while the keys are worked on
+    typename T::Values only;
+    uint32_t only_d[8];
+    int32_t only_ref = kI32Min;
     int32_t top = kI32Min;
     if (threadIdx.x < 16 * (unsigned)ct) lds[threadIdx.x] = kI32Min;
     if (PHASES & 2)
         for (int i = threadIdx.x; i < (16 + T::ACC) * ct; i += blockDim.x) lds[16 * ct + i] = 0;           // sums
     if (PHASES & 1) {
-        if (t.from < t.to) {
+        if (PHASES == 3 && t.from < t.to) {
+            const typename T::Keys keys = t.load_keys(t.from);
+            only = t.load_values(t.from);
+            t.score(keys, t.from, only_d, &only_ref);
+            top = only_ref;
+        }
+        if (PHASES == 1 && t.from < t.to) {
             typename T::Keys now = t.load_keys(t.from);
             for (int32_t at = t.from; at < t.to; at += kTile) {
                 const typename T::Keys next = t.load_keys(min(at + kTile, (t.to - 1) & ~(kTile - 1)));
@@ -379,22 +387,26 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
             for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int h = 0; h < T::PRODUCTS; ++h) acc[b][n][h] = (i32x4){0, 0, 0, 0};
-        const int from_column = min(column, columns - 1);
-        struct Scores { u32x4 a, b; int32_t ref; };
-        auto load_scores = [&](int32_t at) {
-            const u32x4 *o = reinterpret_cast<const u32x4 *>(deltas) + (int64_t)(at / kTile * 4 + p) * 2 * columns + from_column;
-            return (Scores){o[0], o[columns], refs[at / kTile * columns + from_column]};
-        };
-        typename T::Values now = t.load_values(t.from);
-        Scores scores = load_scores(t.from);
-        for (int32_t at = t.from; at < t.to; at += kTile) {
-            const int32_t ahead = min(at + kTile, (t.to - 1) & ~(kTile - 1));
-            const typename T::Values next = t.load_values(ahead);
-            const Scores further = load_scores(ahead);
-            const uint32_t d[8] = {scores.a.x, scores.a.y, scores.a.z, scores.a.w, scores.b.x, scores.b.y, scores.b.z, scores.b.w};
-            t.accumulate(now, d, scores.ref, top, acc, &sum);
-            now = next;
-            scores = further;
+        if (PHASES == 3) {
+            t.accumulate(only, only_d, only_ref, top, acc, &sum);
+        } else {
+            const int from_column = min(column, columns - 1);
+            struct Scores { u32x4 a, b; int32_t ref; };
+            auto load_scores = [&](int32_t at) {
+                const u32x4 *o = reinterpret_cast<const u32x4 *>(deltas) + (int64_t)(at / kTile * 4 + p) * 2 * columns + from_column;
+                return (Scores){o[0], o[columns], refs[at / kTile * columns + from_column]};
+            };
+            typename T::Values now = t.load_values(t.from);
+            Scores scores = load_scores(t.from);
+            for (int32_t at = t.from; at < t.to; at += kTile) {
+                const int32_t ahead = min(at + kTile, (t.to - 1) & ~(kTile - 1));
+                const typename T::Values next = t.load_values(ahead);
+                const Scores further = load_scores(ahead);
+                const uint32_t d[8] = {scores.a.x, scores.a.y, scores.a.z, scores.a.w, scores.b.x, scores.b.y, scores.b.z, scores.b.w};
+                t.accumulate(now, d, scores.ref, top, acc, &sum);
+                now = next;
+                scores = further;
+            }
         }
         // the wavefronts' sums: whole numbers, so the order in which they are added does not matter
         sum += (uint32_t)__shfl_xor((int32_t)sum, 16);
@@ -437,7 +449,8 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
 }
 
 template <int D, int VARIANT, int HALVES, int PHASES>
-__global__ __launch_bounds__(512) void attention_cache_i4_kernel(const CacheAttentionArgs A)
+// (the bound on wavefronts per SIMD keeps the compiler from fetching further ahead than occupancy is worth: 208 registers otherwise)
+__global__ __launch_bounds__(PHASES == 3 ? 1024 : 256, PHASES == 2 && HALVES == 1 ? 3 : 4) void attention_cache_i4_kernel(const CacheAttentionArgs A)
 {
     const uint32_t r1 = div_by(blockIdx.x, A.by_kv_heads), kvh = blockIdx.x - r1 * A.by_kv_heads.d;
     const uint32_t r2 = div_by(r1, A.by_chunks), chunk = r1 - r2 * A.by_chunks.d;

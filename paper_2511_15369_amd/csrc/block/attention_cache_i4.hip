@@ -66,8 +66,8 @@ static CachePlan plan_of(const CacheAttentionCall &c)
     p.pairs = (int64_t)c.n_seq * c.C.kv_heads;
     const int64_t keys = (int64_t)c.max_pages * c.C.page_tokens;           // at most
     p.tiles = (int)((keys + kTile - 1) / kTile);
-    p.whole = keys <= 1024;
-    p.key_waves = p.whole || p.ct == 1 ? 4 : 2;
+    p.whole = keys <= 1024 / p.ct;                        // a tile a wavefront, sixteen wavefronts
+    p.key_waves = p.whole ? std::max(p.tiles, 1) : 4 / p.ct;
     p.splits = 1;
     if (!p.whole) {
         // workgroups enough for the chip, a wavefront with 64 to 1024 keys; with many columns fewer, as each split
@@ -77,7 +77,7 @@ static CachePlan plan_of(const CacheAttentionCall &c)
         p.splits = (int)std::min<int64_t>(std::max(std::max<int64_t>(wanted, least), (int64_t)1), std::min<int64_t>(most, 128));
     }
     const size_t blocks = c.C.dim / 32, stage = std::max(blocks * 4 * 288, (size_t)kTile * c.C.dim / 2 + 256);       // CacheAttention::STAGE
-    p.lds = (size_t)p.key_waves * p.ct * stage + (size_t)p.ct * (32 + c.C.dim / 32 * 512) * 4 + (p.whole ? (size_t)p.tiles * queries * (4 * 32 + 4) : 0);
+    p.lds = (size_t)p.key_waves * p.ct * stage + (size_t)p.ct * (32 + c.C.dim / 32 * 512) * 4;
     const int64_t rows = p.whole ? 0 : p.pairs * columns;
     p.deltas = rows * p.tiles * kTile * 2;
     p.refs = up_to(rows * p.tiles * 4, 16);

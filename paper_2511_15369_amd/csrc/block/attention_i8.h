@@ -296,18 +296,177 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const Atte
     for (int s = 0; s < STEPS; ++s) store_block(out + 32 * s, f, acc_hi[s], acc_lo[s], half, A.P.post);
 }
 
-hipError_t attention_i8_launch_32(const AttentionArgs &a, uint32_t grid, hipStream_t stream);
-hipError_t attention_i8_launch_64(const AttentionArgs &a, uint32_t grid, hipStream_t stream);
-hipError_t attention_i8_launch_96(const AttentionArgs &a, uint32_t grid, hipStream_t stream);
-hipError_t attention_i8_launch_128(const AttentionArgs &a, uint32_t grid, hipStream_t stream);
+// Few queries: a workgroup has 32, and its wavefronts divide the keys, blocks of 32 in turn.  Each keeps to itself until
+// the maxima are joined, and again until the sums are: whole numbers, so their order does not matter.
+constexpr int kFewWaves = 8;
+
+template <int D> struct FewLds {
+    static constexpr int KROW = D + 16, VROW = ValueRow<D>::bytes, stage = 32 * (KROW + VROW);      // of a wavefront
+    static constexpr int acc = D / 32 * 16 * 64 * 4;      // of either half of the weights
+    static constexpr size_t bytes = kFewWaves * stage + 2 * acc + 256;
+};
+
+template <int D, int VARIANT>
+__global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const AttentionArgs A)
+{
+    typedef FewLds<D> L;
+    constexpr int STEPS = D / 32, KROW = L::KROW, VROW = L::VROW;
+    extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+    int32_t *lds_hi = reinterpret_cast<int32_t *>(lds + kFewWaves * L::stage), *lds_lo = lds_hi + L::acc / 4, *lds_top = lds_lo + L::acc / 4;
+    uint32_t *lds_sum = reinterpret_cast<uint32_t *>(lds_top + 32);
+
+    AttentionTile T;
+    if (!attention_tile(A, blockIdx.x, 32, &T)) return;
+    const int32_t nq = T.nq, nk = T.nk;
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t row = T.first + col;
+    const int32_t limit = A.P.causal ? min(max(row + T.diag + 1, 0), nk) : nk;
+    const int32_t most = A.P.causal ? min(max(min(T.first + 32, nq) + T.diag, 0), nk) : nk;        // that any row sees
+    int8_t *stage_k = lds + wave * L::stage, *stage_v = stage_k + 32 * KROW;
+
+    const int8_t *kp = A.k + (int64_t)T.k0 * A.k_stride + T.kvh * D, *vp = A.v + (int64_t)T.k0 * A.v_stride + T.kvh * D;
+    auto load = [&](const int8_t *base, int64_t stride, int32_t at, i32x4 (&r)[STEPS]) {
+        int l = lane;
+        asm volatile("" : "+v"(l));                       // (addresses are made again: kept, they would spill)
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int u = l + 64 * i, key = u / (D / 16);
+            r[i] = *reinterpret_cast<const i32x4_a1 *>(base + (int64_t)min(at + key, nk - 1) * stride + 16 * (u - key * (D / 16)));
+        }
+    };
+    auto put_k = [&](const i32x4 (&r)[STEPS]) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int u = lane + 64 * i, key = u / (D / 16);
+            *reinterpret_cast<i32x4 *>(stage_k + key_row(key) * KROW + 16 * (u - key * (D / 16))) = r[i];
+        }
+    };
+    auto put_v = [&](const i32x4 (&r)[STEPS]) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int u = lane + 64 * i, key = u / (D / 16);
+            *reinterpret_cast<i32x4 *>(stage_v + key * VROW + 16 * (u - key * (D / 16))) = r[i];
+        }
+    };
+    const int32_t from = 32 * wave, step = 32 * kFewWaves;
+    const bool busy = from < most;
+    i32x4 qf[STEPS], kr[STEPS], vr[STEPS];
+    if (busy) {
+        load(kp, A.k_stride, from, kr);
+        load(vp, A.v_stride, from, vr);
+    }
+    {
+        const int8_t *p = A.q + (int64_t)(T.q0 + min(row, nq - 1)) * A.q_stride + T.head * D + 16 * half;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const i32x4_a1 *>(p + 32 * s);
+    }
+    for (int i = threadIdx.x; i < 2 * L::acc / 4; i += 64 * kFewWaves) lds_hi[i] = 0;
+    if (threadIdx.x < 32) {
+        lds_top[threadIdx.x] = kI32Min;
+        lds_sum[threadIdx.x] = 0;
+    }
+    __syncthreads();
+    auto scores = [&]() {
+        i32x16 x = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            x = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const i32x4 *>(stage_k + col * KROW + 32 * s + 16 * half), qf[s], x, 0, 0, 0);
+        return x;
+    };
+    int32_t top = kI32Min;
+    i32x16 x;
+    for (int32_t at = from; at < most; at += step) {
+        wave_lds_fence();
+        put_k(kr);
+        if (at + step < most) load(kp, A.k_stride, at + step, kr);
+        wave_lds_fence();
+        x = scores();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = at + 16 * half + i < limit ? max(top, x[i]) : top;
+    }
+    top = max(top, __shfl_xor(top, 32));
+    if (busy && half == 0) atomicMax(lds_top + col, top);
+    __syncthreads();
+    const int32_t start = score_start(lds_top[col], A.P.shift);
+    if (busy) {
+        i32x16 acc_hi[STEPS], acc_lo[STEPS];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc_hi[s][i] = acc_lo[s][i] = 0;
+        uint32_t sum = 0;
+        const int v_lane = (16 * half + (lane >> 1 & 7)) * VROW + 16 * (lane >> 4 & 1) + 8 * (lane & 1);
+        const bool once = from + step >= most;            // its only block's scores are still there
+        if (!once) load(kp, A.k_stride, from, kr);
+        for (int32_t at = from; at < most; at += step) {
+            wave_lds_fence();
+            put_v(vr);
+            if (!once) put_k(kr);
+            if (at + step < most) {
+                load(kp, A.k_stride, at + step, kr);
+                load(vp, A.v_stride, at + step, vr);
+            }
+            wave_lds_fence();
+            if (!once) x = scores();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = at + 16 * half + i < limit ? x[i] + start : kI32Min;
+            i32x4 hi, lo;
+            weights_of_scores<VARIANT>(x, A.P, &hi, &lo, &sum);
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                const i32x4 vf = values_of_block<VROW>(stage_v + v_lane + 32 * s);
+                acc_hi[s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vf, hi, acc_hi[s], 0, 0, 0);
+                acc_lo[s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(vf, lo, acc_lo[s], 0, 0, 0);
+            }
+        }
+        sum += (uint32_t)__shfl_xor((int32_t)sum, 32);
+        if (half == 0) atomicAdd(lds_sum + col, sum);
+        // 256 hi + lo of up to 508 keys fits 32 bits
+        const bool narrow = most <= 508;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (narrow) {
+                    atomicAdd(lds_lo + (16 * s + i) * 64 + lane, acc_hi[s][i] * 256 + acc_lo[s][i]);
+                } else {
+                    atomicAdd(lds_hi + (16 * s + i) * 64 + lane, acc_hi[s][i]);
+                    atomicAdd(lds_lo + (16 * s + i) * 64 + lane, acc_lo[s][i]);
+                }
+            }
+    }
+    __syncthreads();
+    // a thread's query and four channels: 32 s + 8 i + 4 h
+    for (int u = threadIdx.x; u < 32 * STEPS * 8; u += 64 * kFewWaves) {
+        const int q = u & 31, h = u >> 5 & 1, i = u >> 6 & 3, s = u >> 8;
+        if (T.first + q >= nq) continue;
+        const uint64_t f = floor_div_u64((uint64_t)1 << 54, lds_sum[q]);
+        uint32_t bytes = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int at = (16 * s + 4 * i + j) * 64 + 32 * h + q;
+            bytes |= (uint32_t)(mean_byte(f, (int64_t)lds_hi[at] * 256 + lds_lo[at], 46, A.P.post) & 255) << (8 * j);
+        }
+        *reinterpret_cast<i32_a1 *>(A.out + (int64_t)(T.q0 + T.first + q) * A.out_stride + T.head * D + 32 * s + 8 * i + 4 * h) = (int32_t)bytes;
+    }
+}
+
+hipError_t attention_i8_launch_32(const AttentionArgs &a, bool few, uint32_t grid, hipStream_t stream);
+hipError_t attention_i8_launch_64(const AttentionArgs &a, bool few, uint32_t grid, hipStream_t stream);
+hipError_t attention_i8_launch_96(const AttentionArgs &a, bool few, uint32_t grid, hipStream_t stream);
+hipError_t attention_i8_launch_128(const AttentionArgs &a, bool few, uint32_t grid, hipStream_t stream);
 
 // One file per head dimension instantiates its kernels.
 #define IPTQ_ATTENTION_I8_OF(D)                                                                                          \
-    hipError_t iptq::attention_i8_launch_##D(const AttentionArgs &a, uint32_t grid, hipStream_t stream)                  \
+    hipError_t iptq::attention_i8_launch_##D(const AttentionArgs &a, bool few, uint32_t grid, hipStream_t stream)                  \
     {                                                                                                                    \
         auto kernel = a.P.variant == 0 ? attention_i8_kernel<D, 0> : a.P.variant == 1 ? attention_i8_kernel<D, 1>        \
                                                                                       : attention_i8_kernel<D, 2>;       \
-        launch_kernel(kernel, dim3(grid), dim3(64 * kWaves), 0, stream, a);                                              \
+        if (few)                                                                                                         \
+            kernel = a.P.variant == 0 ? attention_i8_few_kernel<D, 0> : a.P.variant == 1 ? attention_i8_few_kernel<D, 1> \
+                                                                                         : attention_i8_few_kernel<D, 2>; \
+        launch_kernel(kernel, dim3(grid), dim3(64 * (few ? kFewWaves : kWaves)), few ? FewLds<D>::bytes : 0, stream, a); \
         return take_launch_status();                                                                                     \
     }
 

@@ -15,14 +15,19 @@ hipError_t attention_i8_dispatch(const AttentionCall &c, hipStream_t stream)
     a.by_kv_heads = div_of((uint32_t)c.kv_heads);
     a.by_group = div_of((uint32_t)(c.heads / c.kv_heads));
     a.by_seq = div_of((uint32_t)c.n_seq);
-    a.tiles = ((uint32_t)c.max_q + kQueries - 1) / kQueries;
     a.P = c.P;
-    const uint32_t grid = a.tiles * (uint32_t)c.n_seq * (uint32_t)c.heads;      // below 2^31: checked
+    // Workgroups of 128 queries, or of 32 with their keys divided over the wavefronts where the former do not reach every
+    // compute unit.
+    const uint32_t pairs = (uint32_t)c.n_seq * (uint32_t)c.heads;
+    a.tiles = ((uint32_t)c.max_q + kQueries - 1) / kQueries;
+    const bool few = (int64_t)a.tiles * pairs < 256;
+    if (few) a.tiles = ((uint32_t)c.max_q + 31) / 32;
+    const uint32_t grid = a.tiles * pairs;                // below 2^31: checked
     switch (c.dim) {
-    case 32: return attention_i8_launch_32(a, grid, stream);
-    case 64: return attention_i8_launch_64(a, grid, stream);
-    case 96: return attention_i8_launch_96(a, grid, stream);
-    default: return attention_i8_launch_128(a, grid, stream);
+    case 32: return attention_i8_launch_32(a, few, grid, stream);
+    case 64: return attention_i8_launch_64(a, few, grid, stream);
+    case 96: return attention_i8_launch_96(a, few, grid, stream);
+    default: return attention_i8_launch_128(a, few, grid, stream);
     }
 }
 

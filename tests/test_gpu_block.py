@@ -71,13 +71,14 @@ def _packed(rng, q_lens, k_lens, heads, kv_heads, dim, p, fused=True, max_q=None
 @pytest.mark.parametrize("dim", [32, 64, 96, 128])
 @pytest.mark.parametrize("variant", [0, 1, 2])
 @pytest.mark.parametrize("causal", [0, 1])
-def test_packed_lengths(dim, variant, causal):
+@pytest.mark.parametrize("heads", [6, 27])                # 10 sequences of up to two tiles: 120 tiles of 128 queries, and 540
+def test_packed_lengths(dim, variant, causal, heads):
     """Lengths around the tiles' edges, sequences without queries, without keys, with fewer keys than queries."""
-    rng = np.random.default_rng([dim, variant, causal])
+    rng = np.random.default_rng([dim, variant, causal, heads])
     q_lens = [1, 0, 31, 33, 64, 129, 65, 5, 130, 1]
     k_lens = [1, 4, 31, 40, 63, 129, 257, 0, 100, 300]
     p = _attention(rng, dim, 27 * 27 * dim ** 0.5, variant, causal, keys=100)
-    _packed(rng, q_lens, k_lens, 6, 2, dim, p, offset=int(rng.integers(0, 16)))
+    _packed(rng, q_lens, k_lens, heads, heads // 3, dim, p, offset=int(rng.integers(0, 16)))
 
 
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (3, 3), (8, 1), (5, 5), (40, 8), (12, 4)])
@@ -88,11 +89,21 @@ def test_heads(heads, kv_heads, dim):
         _packed(rng, [70, 3, 40], [70, 9, 41], heads, kv_heads, dim, _attention(rng, dim, 27 * 27 * dim ** 0.5, keys=40), fused)
 
 
-@pytest.mark.parametrize("n,dim,variant", [(1000, 128, 0), (1537, 64, 1), (2111, 32, 2), (700, 96, 1)])
+@pytest.mark.parametrize("n,dim,variant,heads", [(1000, 128, 0, 2), (1537, 64, 1, 2), (2111, 32, 2, 2), (700, 96, 1, 2), (1000, 128, 1, 32), (1537, 64, 0, 20),
+                                                 (1999, 32, 1, 16), (700, 96, 2, 48), (641, 128, 2, 48)])
 @pytest.mark.parametrize("causal", [0, 1])
-def test_long_prompts(n, dim, variant, causal):
+def test_long_prompts(n, dim, variant, heads, causal):
     rng = np.random.default_rng([n, causal])
-    _packed(rng, [n], [n + (37 if causal else 0)], 2, 1, dim, _attention(rng, dim, 27 * 27 * dim ** 0.5, variant, causal, keys=n))
+    _packed(rng, [n], [n + (37 if causal else 0)], heads, heads // 2, dim, _attention(rng, dim, 27 * 27 * dim ** 0.5, variant, causal, keys=n))
+
+
+@pytest.mark.parametrize("n,k", [(1, 1), (3, 508), (5, 509), (1, 3000), (32, 255), (33, 256), (2, 257), (4, 2049)])
+def test_few_queries_of_many_keys(n, k):
+    """Keys divided over wavefronts: around one block each, and where a sum no longer fits with its upper half in one."""
+    rng = np.random.default_rng([n, k])
+    for dim in (32, 64, 96, 128):
+        for causal in (0, 1):
+            _packed(rng, [n], [k], 2, 1, dim, _attention(rng, dim, 27 * 27 * dim ** 0.5, 1, causal, keys=k))
 
 
 def test_more_queries_than_max_q_and_wild_offsets_stay():
@@ -110,6 +121,8 @@ def test_extreme_scores_and_scales(i0, sigma):
             p = _attention(rng, 128, 27 * 27 * 11.0, variant, 1, i0)
             p.score_shift = shift
             _packed(rng, [40], [67], 2, 1, 128, p, sigma=sigma)
+            if shift == 5:
+                _packed(rng, [40] * 6, [67] * 6, 48, 1, 32, p, sigma=sigma)
 
 
 def test_bytes_at_their_ends():
@@ -119,10 +132,11 @@ def test_bytes_at_their_ends():
     for q, k, v in ((-128, -128, -128), (-128, 127, 127), (0, 0, -128), (127, 127, 127)):
         for i0 in (1019, 1018):                  # 1019 << 5 is the largest weight but 31
             p = ob.Attention(1, i0, 5, 4, 0, Dyadic(1, 8, 0, -128, 127))
-            t = [torch.full((m, 1, 128), x, dtype=torch.int8, device="cuda") for m, x in ((40, q), (n, k), (n, v))]
-            out = torch.empty_like(t[0])
-            ip.attention_i8(*t, None, None, 1, 40, out, _params(p))
-            assert torch.all(out == v)                   # (rounding down by f may take a unit of 2^-8, never half of one)
+            for heads in (1, 256):
+                t = [torch.full((m, h, 128), x, dtype=torch.int8, device="cuda") for m, h, x in ((40, heads, q), (n, 1, k), (n, 1, v))]
+                out = torch.empty_like(t[0])
+                ip.attention_i8(*t, None, None, 1, 40, out, _params(p))
+                assert torch.all(out == v)               # (rounding down by f may take a unit of 2^-8, never half of one)
 
 
 def test_longest_keys():
@@ -144,7 +158,7 @@ def test_longest_keys():
 def test_equal_lengths_without_offsets():
     import torch
     rng = np.random.default_rng(6)
-    for n, lq, lk in ((3, 197, 197), (5, 49, 49), (2, 1, 30), (4, 16, 0)):
+    for n, lq, lk in ((3, 197, 197), (5, 49, 49), (2, 1, 30), (4, 16, 0), (70, 49, 49), (65, 16, 0)):
         q, k, v = (rng.integers(-90, 90, (n * m, 4, 64)).astype(np.int8) for m in (lq, lk, lk))
         p = _attention(rng, 64, 52 * 52 * 8.0, causal=0, keys=lk)
         out = torch.full((n * lq, 4, 64), 9, dtype=torch.int8, device="cuda")
@@ -282,6 +296,13 @@ def test_cache_attention_columns(heads, kv_heads, t):
     rng = np.random.default_rng([heads, t])
     for causal in (0, 1):
         _attend(rng, [300, 70, 5], heads, kv_heads, 128, 32, t, _attention(rng, 128, _spread(128), 1, causal, cache=True))
+
+
+@pytest.mark.parametrize("heads,n", [(4, 1023), (4, 1024), (4, 1025), (40, 512), (40, 513), (40, 1024), (24, 1024), (4, 64), (4, 65)])
+def test_cache_attention_at_the_limits_of_one_workgroup(heads, n):
+    rng = np.random.default_rng([heads, n])
+    for dim in (32, 64, 96, 128):
+        _attend(rng, [n, 3, n - 1], heads, 2, dim, 16, 1, _attention(rng, dim, _spread(dim), 2, 1, keys=n, cache=True))
 
 
 @pytest.mark.parametrize("n,dim,t,heads", [(1500, 128, 1, 4), (2600, 64, 2, 8), (5000, 128, 4, 8), (9000, 32, 1, 2), (20011, 96, 1, 2)])
