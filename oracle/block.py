@@ -57,6 +57,11 @@ def mean(acc, total, shift, post):
     return dyadic((f * acc) >> shift, post).astype(np.int8)
 
 
+def _product(a, b):
+    """Whole numbers: every partial sum stays below 2^53, where doubles hold them exactly."""
+    return (a.astype(np.float64) @ b.astype(np.float64)).astype(np.int64)
+
+
 def attention(q, k, v, p, seen=None):
     """One sequence: q [nq, heads, d], k and v [nk, kv heads, d] int8."""
     (nq, heads, d), (nk, kv_heads, _) = q.shape, k.shape
@@ -65,9 +70,9 @@ def attention(q, k, v, p, seen=None):
     out = np.zeros(q.shape, np.int8)
     for h in range(heads):
         g = h // (heads // kv_heads)
-        x = q[:, h].astype(np.int64) @ k[:, g].astype(np.int64).T
+        x = _product(q[:, h], k[:, g].T)
         w = weights(x, seen, p)
-        out[:, h] = mean(w @ v[:, g].astype(np.int64), w.sum(1), 46, p.post)
+        out[:, h] = mean(_product(w, v[:, g]), w.sum(1), 46, p.post)
     return out
 
 
@@ -138,10 +143,10 @@ def attention_cache(q, cache, pages, lengths, q_tokens, p):
         for h in range(heads):
             g = h // (heads // kv_heads)
             spread = lambda a: np.repeat(a.astype(np.int64), GROUP, 1)[:, :d]  # noqa: E731
-            x = q[rows, h].astype(np.int64) @ (unpack(kc[at, g, pos]) * spread(ks[at, g, pos])).T
+            x = _product(q[rows, h], (unpack(kc[at, g, pos]) * spread(ks[at, g, pos])).T)
             w = weights(x, keep, p)
             c = unpack(vc.transpose(0, 1, 3, 2)[at, g, pos])
-            acc = np.concatenate([rshr_round(w * vs[at, g, pos][:, j].astype(np.int64), 7) @ c[:, j * GROUP:(j + 1) * GROUP]
+            acc = np.concatenate([_product(rshr_round(w * vs[at, g, pos][:, j].astype(np.int64), 7), c[:, j * GROUP:(j + 1) * GROUP])
                                   for j in range(groups(d))], 1)
             out[rows, h] = mean(acc, w.sum(1), 39, p.post)
     return out

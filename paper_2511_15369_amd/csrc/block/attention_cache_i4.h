@@ -162,15 +162,17 @@ struct CacheAttention {
     }
     // The block and the channel pair (of 16) whose tokens the lane loads: a page's tokens of a pair lie side by side, so
     // the lanes of a quad take blocks of the same page and then further pairs.
-    IPTQ_DEV int value_block() const { return A.C.page_log >= 6 ? lane & 3 : A.C.page_log == 5 ? (lane & 1) | lane >> 5 << 1 : lane >> 4; }
-    IPTQ_DEV int value_pair() const { return A.C.page_log >= 6 ? lane >> 2 : A.C.page_log == 5 ? lane >> 1 & 15 : lane & 15; }
+    IPTQ_DEV int value_block(int lane) const { return A.C.page_log >= 6 ? lane & 3 : A.C.page_log == 5 ? (lane & 1) | lane >> 5 << 1 : lane >> 4; }
+    IPTQ_DEV int value_pair(int lane) const { return A.C.page_log >= 6 ? lane >> 2 : A.C.page_log == 5 ? lane >> 1 & 15 : lane & 15; }
     IPTQ_DEV Values load_values(int32_t at) const
     {
         Values v;
         const CacheDev &C = A.C;
-        const int first = (at - from) >> 4, mask = C.page_tokens - 1, block = value_block();
+        int l = lane;
+        asm volatile("" : "+v"(l));                       // (made again each time: kept, it may spill)
+        const int first = (at - from) >> 4, mask = C.page_tokens - 1, block = value_block(l);
         const int64_t head_at = (int64_t)max(__shfl(page_of_block, first + block), 0) * C.kv_heads + kvh;
-        const uint8_t *src = C.v_codes + (head_at * PAIRS + value_pair()) * C.page_tokens + ((at + 16 * block) & mask);
+        const uint8_t *src = C.v_codes + (head_at * PAIRS + value_pair(l)) * C.page_tokens + ((at + 16 * block) & mask);
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) v.codes[b] = *reinterpret_cast<const u32x4 *>(src + (int64_t)(16 * b) * C.page_tokens);
         const int64_t step_row = ((int64_t)max(__shfl(page_of_block, first + p), 0) * C.kv_heads + kvh) * C.page_tokens + ((at + 16 * p) & mask);
@@ -180,7 +182,9 @@ struct CacheAttention {
     }
     IPTQ_DEV void stage_values(const Values &v) const
     {
-        const int at = value_block() * 288 + value_pair() * 16;
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        const int at = value_block(l) * 288 + value_pair(l) * 16;
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) *reinterpret_cast<u32x4 *>(stage + b * kValueBlock + at) = v.codes[b];
         wave_lds_fence();
@@ -289,11 +293,10 @@ struct CacheAttention {
 };
 
 // 8 sums of a channel pair block -> 8 output bytes
-IPTQ_DEV void store_means(int8_t *out, uint64_t f, const int64_t (&acc)[8], const DyadicDev &post)
+IPTQ_DEV void store_means(int8_t *out, uint64_t f, const int64_t (&acc)[8], const AttentionDev &P)
 {
-    uint32_t w[2] = {0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)(mean_byte(f, acc[i], 39, post) & 255) << (8 * (i & 3));
+    const int64_t a[4] = {acc[0], acc[1], acc[2], acc[3]}, b[4] = {acc[4], acc[5], acc[6], acc[7]};
+    const uint32_t w[2] = {mean_bytes(f, a, 39, P.post_shift, P.post), mean_bytes(f, b, 39, P.post_shift, P.post)};
     typedef u32x2_t __attribute__((aligned(1))) u32x2_any;
     *reinterpret_cast<u32x2_any *>(out) = (u32x2_t){w[0], w[1]};
 }
@@ -437,7 +440,7 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
         const int channel = 32 * b + 8 * (l >> 4);
         if (PHASES == 3) {
             const uint32_t token = div_by(x, A.by_group), head = kvh * (uint32_t)A.group + (x - token * (uint32_t)A.group);
-            store_means(A.out + t.q_row(token) * A.out_stride + head * D + channel, floor_div_u64((uint64_t)1 << 54, s), v, A.P.post);
+            store_means(A.out + t.q_row(token) * A.out_stride + head * D + channel, floor_div_u64((uint64_t)1 << 54, s), v, A.P);
         } else {
             const int64_t at = (pair * A.splits + split) * A.columns + x;
             i32x4 *o = reinterpret_cast<i32x4 *>(A.partial + at * D + channel);

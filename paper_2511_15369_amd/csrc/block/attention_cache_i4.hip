@@ -42,7 +42,7 @@ __global__ __launch_bounds__(256) void attention_cache_i4_join_kernel(const Cach
     for (int j = 0; j < 8; ++j) v[j] = parts[0][unit][j] + parts[1][unit][j] + parts[2][unit][j] + parts[3][unit][j];
     const uint64_t f = floor_div_u64((uint64_t)1 << 54, totals[0] + totals[1] + totals[2] + totals[3]);
     const uint32_t token = div_by(column, A.by_group), head = kvh * (uint32_t)A.group + (column - token * (uint32_t)A.group);
-    store_means(A.out + ((int64_t)seq * A.q_tokens + token) * A.out_stride + head * dim + 8 * unit, f, v, A.P.post);
+    store_means(A.out + ((int64_t)seq * A.q_tokens + token) * A.out_stride + head * dim + 8 * unit, f, v, A.P);
 }
 
 struct CachePlan {

@@ -19,6 +19,17 @@
 
 namespace iptq {
 
+// The output step where the means are below 2^15 in magnitude, as those of int8 values with eight fractional bits are: products
+// below 2^30 (from s = 31 on all of them round to 0).
+struct NarrowPost {
+    int32_t m, s, rnd;
+};
+inline NarrowPost narrow_post_of(int32_t m, int32_t s)
+{
+    if (s > 30) return {0, 0, 0};
+    return {m, s, s > 0 ? 1 << (s - 1) : 0};
+}
+
 struct AttentionArgs {
     const int8_t *q, *k, *v;
     int8_t *out;
@@ -28,6 +39,7 @@ struct AttentionArgs {
     DivDev by_kv_heads, by_group, by_seq;                 // workgroup number -> kv head, head of its group, sequence, tile
     uint32_t tiles;
     AttentionDev P;
+    NarrowPost post;
 };
 
 constexpr int kWaves = 4;             // 32 queries each
@@ -119,18 +131,34 @@ IPTQ_DEV i32x4 values_of_block(const int8_t *src)
     return (i32x4){a.x, a.y, b.x, b.y};
 }
 
-// 16 outputs of a 32-channel block: floor(2^54 / sum) times the sums, 46 bits down, requantized.
-IPTQ_DEV void store_block(int8_t *out, uint64_t f, const i32x16 &hi, const i32x16 &lo, int half, const DyadicDev &post)
+// floor(2^54 / sum) times four sums, 46 bits down, requantized.  NARROW: the sum of the weights is below 2^24, that of the weighted
+// values below 2^31 then, and f = 2^32 fh + fl with a signed fl has two products in place of five.
+template <bool NARROW>
+IPTQ_DEV int32_t means_of(uint64_t f, const int32_t (&hi)[4], const int32_t (&lo)[4], const AttentionArgs &A)
+{
+    const int32_t fl = (int32_t)f, fh = (int32_t)((int64_t)(f - (uint64_t)(int64_t)fl) >> 32);
+    int32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        int32_t o;
+        if (NARROW) {
+            const int32_t acc = (hi[i] << 8) + lo[i];
+            o = (fh * acc + __mulhi(fl, acc)) >> 14;
+        } else {
+            o = mean_of(f, (int64_t)hi[i] * 256 + lo[i], 46);
+        }
+        c[i] = clamp_i32(((__mul24(o, A.post.m) + A.post.rnd) >> A.post.s) + A.P.post.zp, A.P.post.qmin, A.P.post.qmax);
+    }
+    return (int32_t)four_bytes(c);
+}
+// 16 outputs of a 32-channel block
+template <bool NARROW>
+IPTQ_DEV void store_block(int8_t *out, uint64_t f, const i32x16 &hi, const i32x16 &lo, int half, const AttentionArgs &A)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t bytes = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t acc = (int64_t)hi[4 * i + j] * 256 + lo[4 * i + j];
-            bytes |= (uint32_t)(mean_byte(f, acc, 46, post) & 255) << (8 * j);
-        }
-        *reinterpret_cast<i32_a1 *>(out + 8 * i + 4 * half) = (int32_t)bytes;
+        const int32_t h[4] = {hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]}, l[4] = {lo[4 * i], lo[4 * i + 1], lo[4 * i + 2], lo[4 * i + 3]};
+        *reinterpret_cast<i32_a1 *>(out + 8 * i + 4 * half) = means_of<NARROW>(f, h, l, A);
     }
 }
 
@@ -292,8 +320,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const Atte
     if (row >= nq) return;
     const uint64_t f = floor_div_u64((uint64_t)1 << 54, sum);
     int8_t *out = A.out + (int64_t)(T.q0 + row) * A.out_stride + T.head * D;
+    if (__all(sum < 1u << 24)) {
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) store_block(out + 32 * s, f, acc_hi[s], acc_lo[s], half, A.P.post);
+        for (int s = 0; s < STEPS; ++s) store_block<true>(out + 32 * s, f, acc_hi[s], acc_lo[s], half, A);
+    } else {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) store_block<false>(out + 32 * s, f, acc_hi[s], acc_lo[s], half, A);
+    }
 }
 
 // Few queries: a workgroup has 32, and its wavefronts divide the keys, blocks of 32 in turn.  Each keeps to itself until
@@ -442,13 +475,15 @@ __global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const 
         const int q = u & 31, h = u >> 5 & 1, i = u >> 6 & 3, s = u >> 8;
         if (T.first + q >= nq) continue;
         const uint64_t f = floor_div_u64((uint64_t)1 << 54, lds_sum[q]);
-        uint32_t bytes = 0;
+        int32_t hi[4], lo[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int at = (16 * s + 4 * i + j) * 64 + 32 * h + q;
-            bytes |= (uint32_t)(mean_byte(f, (int64_t)lds_hi[at] * 256 + lds_lo[at], 46, A.P.post) & 255) << (8 * j);
+            hi[j] = lds_hi[at];
+            lo[j] = lds_lo[at];
         }
-        *reinterpret_cast<i32_a1 *>(A.out + (int64_t)(T.q0 + T.first + q) * A.out_stride + T.head * D + 32 * s + 8 * i + 4 * h) = (int32_t)bytes;
+        *reinterpret_cast<i32_a1 *>(A.out + (int64_t)(T.q0 + T.first + q) * A.out_stride + T.head * D + 32 * s + 8 * i + 4 * h) =
+            most <= 508 ? means_of<true>(f, hi, lo, A) : means_of<false>(f, hi, lo, A);
     }
 }
 

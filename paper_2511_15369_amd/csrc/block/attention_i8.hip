@@ -16,6 +16,7 @@ hipError_t attention_i8_dispatch(const AttentionCall &c, hipStream_t stream)
     a.by_group = div_of((uint32_t)(c.heads / c.kv_heads));
     a.by_seq = div_of((uint32_t)c.n_seq);
     a.P = c.P;
+    a.post = narrow_post_of(c.P.post.m, c.P.post.s);
     // Workgroups of 128 queries, or of 32 with their keys divided over the wavefronts where the former do not reach every
     // compute unit.
     const uint32_t pairs = (uint32_t)c.n_seq * (uint32_t)c.heads;

@@ -18,7 +18,6 @@ typedef short i16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kGroup = 64;            // channels that share one step of the 4-bit cache
-constexpr int kGroupsMost = 2;        // head dimensions go up to 128
 
 // Unsigned division by a run-time constant (the compiler's own goes through floating point).
 struct DivDev {
@@ -33,6 +32,24 @@ inline DivDev div_of(uint32_t d)      // 1 <= d, dividends below 2^31
 }
 IPTQ_HD uint32_t div_by(uint32_t n, const DivDev &D) { return D.d == 1 ? n : mulhi_u32(n, D.magic) >> D.sh; }
 
+// rshr_round(x m, s) for |x| < 2^31, |m| < 2^15.  fast (s >= 16): one multiplication and a shift of its upper half (mul and rnd
+// moved up to where the result's lowest bit is the upper half's), and the result fits 32 bits.
+struct ShiftDev {
+    int32_t m, s;
+    int32_t mul, sh;
+    int64_t rnd;
+};
+inline ShiftDev shift_of(int32_t m, int32_t s, bool fast)
+{
+    ShiftDev v = {m, s, 0, 0, s > 0 ? (int64_t)1 << (s - 1) : 0};
+    if (fast) {
+        v.mul = (int32_t)((uint32_t)m << (s <= 32 ? 32 - s : 0));
+        v.sh = s > 32 ? s - 32 : 0;
+        if (s <= 32) v.rnd = (int64_t)1 << 31;
+    }
+    return v;
+}
+
 // Constants of an attention's exponentials and of its output step.
 struct AttentionDev {
     int32_t variant, i0, i0n, n_shift;
@@ -43,6 +60,7 @@ struct AttentionDev {
     int32_t shift;                    // scores are brought to i0's scale by a rounding shift
     int32_t causal;
     DyadicDev post;
+    ShiftDev post_shift;
 };
 
 struct AttentionCall {
@@ -232,11 +250,43 @@ IPTQ_DEV void split_weights(uint32_t w01, uint32_t w23, uint32_t *hi, uint32_t *
     *lo = __builtin_amdgcn_perm(w23, w01, 0x06040200u);
 }
 
-// One output byte: floor(2^54 / total) times the sum of weighted values, shifted, requantized.
-IPTQ_DEV int32_t mean_byte(uint64_t f, int64_t acc, int shift, const DyadicDev &post)
+IPTQ_DEV int32_t shifted_fast(int32_t x, const ShiftDev &S) { return (int32_t)(((int64_t)x * S.mul + S.rnd) >> 32) >> S.sh; }
+IPTQ_DEV int64_t shifted(int32_t x, const ShiftDev &S) { return ((int64_t)x * S.m + S.rnd) >> S.s; }
+
+// clamp(rshr_round(x m, s) + zp, qmin, qmax)
+template <bool FAST>
+IPTQ_DEV int32_t code_of(int32_t x, const ShiftDev &S, const DyadicDev &P)
 {
-    const int64_t o = (int64_t)(f * (uint64_t)acc) >> shift;
-    return requant_dev<false>((int32_t)o, post.m, post.s, post.zp, post.qmin, post.qmax);
+    if (FAST) return clamp_i32(shifted_fast(x, S) + P.zp, P.qmin, P.qmax);      // (|x m| < 2^46: 2^30 at most, and zp 2^24)
+    int64_t v = shifted(x, S) + P.zp;
+    v = v < P.qmin ? P.qmin : v > P.qmax ? P.qmax : v;
+    return (int32_t)v;
+}
+IPTQ_DEV uint32_t four_bytes(const int32_t (&c)[4])
+{
+    const uint32_t a = __builtin_amdgcn_perm((uint32_t)c[1], (uint32_t)c[0], 0x0c0c0400u);
+    return __builtin_amdgcn_perm((uint32_t)c[3], (uint32_t)c[2], 0x04000c0cu) | a;
+}
+
+// (f * acc) >> shift for 32 <= shift, the product below 2^63 in magnitude: the mean of the weighted values
+IPTQ_DEV int32_t mean_of(uint64_t f, int64_t acc, int shift)
+{
+    const uint32_t fl = (uint32_t)f, fh = (uint32_t)(f >> 32), al = (uint32_t)acc, ah = (uint32_t)((uint64_t)acc >> 32);
+    const uint32_t hi = __umulhi(fl, al) + fl * ah + fh * al;
+    return (int32_t)hi >> (shift - 32);
+}
+// Four means of a query's outputs -> their bytes.
+IPTQ_DEV uint32_t mean_bytes(uint64_t f, const int64_t (&acc)[4], int shift, const ShiftDev &S, const DyadicDev &P)
+{
+    int32_t c[4];
+    if (S.s >= 16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = code_of<true>(mean_of(f, acc[i], shift), S, P);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = code_of<false>(mean_of(f, acc[i], shift), S, P);
+    }
+    return four_bytes(c);
 }
 
 }  // namespace iptq

@@ -15,35 +15,6 @@ constexpr int32_t kResidualMost = (1 << 23) - 1;
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef i16x4 __attribute__((aligned(2))) i16x4_a2;
 
-// rshr_round(x m, s) for |x| < 2^31, |m| < 2^15.  FAST: s >= 16, one multiplication and a shift of its upper half (mul
-// and rnd moved up to where the result's lowest bit is the upper half's), and the result fits 32 bits.
-struct ShiftDev {
-    int32_t m, s;
-    int32_t mul, sh;
-    int64_t rnd;
-};
-static ShiftDev shift_of(int32_t m, int32_t s)
-{
-    return {m, s, s >= 16 ? (int32_t)((uint32_t)m << (s <= 32 ? 32 - s : 0)) : 0, s > 32 ? s - 32 : 0, s >= 16 ? pre_rnd_of(s) : s > 0 ? (int64_t)1 << (s - 1) : 0};
-}
-IPTQ_DEV int32_t shifted_fast(int32_t x, const ShiftDev &S) { return (int32_t)(((int64_t)x * S.mul + S.rnd) >> 32) >> S.sh; }
-IPTQ_DEV int64_t shifted(int32_t x, const ShiftDev &S) { return ((int64_t)x * S.m + S.rnd) >> S.s; }
-
-// clamp(rshr_round(x m, s) + zp, qmin, qmax)
-template <bool FAST>
-IPTQ_DEV int32_t code_of(int32_t x, const ShiftDev &S, const DyadicDev &P)
-{
-    if (FAST) return clamp_i32(shifted_fast(x, S) + P.zp, P.qmin, P.qmax);      // (|x m| < 2^46: 2^30 at most, and zp 2^24)
-    int64_t v = shifted(x, S) + P.zp;
-    v = v < P.qmin ? P.qmin : v > P.qmax ? P.qmax : v;
-    return (int32_t)v;
-}
-IPTQ_DEV uint32_t four_bytes(const int32_t (&c)[4])
-{
-    const uint32_t a = __builtin_amdgcn_perm((uint32_t)c[1], (uint32_t)c[0], 0x0c0c0400u);
-    return __builtin_amdgcn_perm((uint32_t)c[3], (uint32_t)c[2], 0x04000c0cu) | a;
-}
-
 struct RmsnormArgs {
     const int32_t *x, *residual;
     int32_t *residual_out;
@@ -226,19 +197,13 @@ hipError_t rmsnorm_i32_dispatch(const RmsnormCall &c, hipStream_t stream)
     RmsnormArgs a;
     a.x = c.x; a.residual = c.residual; a.residual_out = c.residual_out; a.gain = c.gain; a.out = c.out; a.row_scales = c.row_scales;
     a.rows = (int32_t)c.rows; a.cols = c.cols; a.eps_sum = c.eps_sum; a.root_cols = c.root_cols;
-    a.in = shift_of(c.in_m, c.in_s);
-    a.post = shift_of(c.post.m, c.post.s);
     a.p = c.post;
-    const bool fast = c.in_s >= 16 && (c.post.s >= 16 || c.row_scales);
+    const bool fast = c.cols >= 4 && c.in_s >= 16 && (c.post.s >= 16 || c.row_scales);
+    a.in = shift_of(c.in_m, c.in_s, fast);
+    a.post = shift_of(c.post.m, c.post.s, fast && c.post.s >= 16);
     if (c.cols < 4) {
-        a.in.rnd = c.in_s > 0 ? (int64_t)1 << (c.in_s - 1) : 0;            // (the general form of both steps)
-        a.post.rnd = c.post.s > 0 ? (int64_t)1 << (c.post.s - 1) : 0;
         launch_kernel(rmsnorm_narrow_kernel, dim3(((uint32_t)c.rows + 255) / 256), dim3(256), 0, stream, a);
         return take_launch_status();
-    }
-    if (!fast) {
-        a.in.rnd = c.in_s > 0 ? (int64_t)1 << (c.in_s - 1) : 0;
-        a.post.rnd = c.post.s > 0 ? (int64_t)1 << (c.post.s - 1) : 0;
     }
     const int chunks = (c.cols + 3) / 4;
     // Wavefronts per row: one up to 1024 values; beyond, four with up to eight chunks a lane while there are rows enough to fill the
@@ -306,7 +271,7 @@ hipError_t requant_rows_dispatch(const int32_t *in, const int32_t *row_scales, i
     RequantRowsArgs a;
     a.rnd = row_shift > 0 ? (int64_t)1 << (row_shift - 1) : 0;
     a.cols = cols; a.row_shift = row_shift;
-    a.S = shift_of(P.m, P.s);
+    a.S = shift_of(P.m, P.s, P.s >= 16);
     a.P = P;
     const int width = cols < 4 ? 1 : 4;
     const int64_t per_row = (cols + width - 1) / width, most_rows = (((int64_t)1 << 30) / per_row);

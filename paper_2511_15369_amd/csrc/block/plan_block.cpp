@@ -43,6 +43,7 @@ static int plan_attention(const iptq_attention_params_t *p, int32_t most_shift, 
     out->variant = p->variant; out->i0 = p->i0; out->i0n = d.i0n; out->n_shift = p->n_shift;
     out->d_clamp = d.d_clamp; out->div8 = d.div8; out->d2_magic = d.d2_magic; out->d2_sh = d.d2_sh;
     out->shift = p->score_shift; out->causal = p->causal;
+    out->post_shift = shift_of(p->post.m, p->post.s, p->post.s >= 16);
     return plan_requant(&p->post, 1, &out->post);
 }
 
