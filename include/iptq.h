@@ -363,7 +363,7 @@ typedef struct {
  * max_q: the longest sequence's number of queries; those beyond it, and rows of d_out that belong to no sequence, are left
  * as they were.  Offsets are read on the device and clamped to [0, tokens]; a sequence of more than
  * IPTQ_KEYS_MAX keys is not served, its rows are left as they were.  n_seq, max_q or q_tokens 0: a no-op.
- * d_out must not overlap an input.  max_q (rounded up to 32) / 32 * n_seq * heads < 2^31.
+ * d_out must not overlap an input.  min(max_q, q_tokens) (rounded up to 32) / 32 * n_seq * heads < 2^31.
  */
 #define IPTQ_KEYS_MAX 65536
 int iptq_attention_i8(const int8_t *d_q, int64_t q_stride, const int8_t *d_k, int64_t k_stride, const int8_t *d_v, int64_t v_stride,
@@ -390,7 +390,7 @@ typedef struct {
  * Stores `tokens` rows of keys and values (int8, as in iptq_attention_i8) into the cache: row i goes to
  * slot d_slots[i] = page * page_tokens + position (int32, device).  A slot outside [0, n_pages * page_tokens) is skipped
  * (padding: -1).  No two rows of a call may name the same slot (what that slot then holds is not
- * specified; nothing else is touched).  tokens / 64 (rounded up) * kv_heads < 2^31.
+ * specified; nothing else is touched).  tokens / 64 (rounded up) * kv_heads < 2^24.
  */
 int iptq_cache_store_i4(const iptq_cache_i4_t *cache /*host*/, const int8_t *d_k, int64_t k_stride, const int8_t *d_v, int64_t v_stride,
                         const int32_t *d_slots, int64_t tokens, void *stream);
@@ -407,7 +407,8 @@ int iptq_cache_store_i4(const iptq_cache_i4_t *cache /*host*/, const int8_t *d_k
  *   of it fit a signed byte; o_d = (f * sum_j u_j c'_jd) >> 39, seven times the mean with eight fractional bits; step 4.
  * Lengths are clamped to [0, max_pages * page_tokens]; tokens in a page outside [0, n_pages) count as masked and
  * are not read.  A query that sees no key gives the step 4 of 0.  1 <= q_tokens <= IPTQ_CACHE_QUERIES_MAX,
- * max_pages * page_tokens <= IPTQ_CACHE_KEYS_MAX, n_seq * q_tokens * heads < 2^24.
+ * max_pages * page_tokens <= IPTQ_CACHE_KEYS_MAX, n_seq * q_tokens * heads < 2^24, and times max_pages * page_tokens / 1024
+ * (rounded up) too.
  * d_work: iptq_attention_cache_i4_workspace bytes (16-byte aligned; IPTQ_ERR_WORKSPACE if there are fewer; it may be
  * NULL where that is 0).  Its contents need no preparation and mean nothing afterwards; calls that may run at the same time need
  * one each.  d_out and d_work must not overlap an input or each other.

@@ -66,7 +66,8 @@ static CachePlan plan_of(const CacheAttentionCall &c)
     p.pairs = (int64_t)c.n_seq * c.C.kv_heads;
     const int64_t keys = (int64_t)c.max_pages * c.C.page_tokens;           // at most
     p.tiles = (int)((keys + kTile - 1) / kTile);
-    p.whole = keys <= 1024 / p.ct;                        // a tile a wavefront, sixteen wavefronts
+    // a tile a wavefront, sixteen wavefronts
+    p.whole = keys <= 1024 / p.ct && p.pairs * p.chunks <= (int64_t)kLaunchMost;
     p.key_waves = p.whole ? std::max(p.tiles, 1) : 4 / p.ct;
     p.splits = 1;
     if (!p.whole) {
@@ -89,6 +90,7 @@ static CachePlan plan_of(const CacheAttentionCall &c)
 
 int64_t attention_cache_i4_workspace_bytes(const CacheAttentionCall &c)
 {
+    if (c.n_seq == 0) return 0;
     const CachePlan p = plan_of(c);
     return p.deltas + p.refs + p.tops + p.partial + p.sums;
 }

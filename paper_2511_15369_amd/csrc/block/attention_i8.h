@@ -38,6 +38,7 @@ struct AttentionArgs {
     int32_t q_tokens, k_tokens, q_len, k_len, max_q;      // q_len, k_len: of every sequence where there are no offsets
     DivDev by_kv_heads, by_group, by_seq;                 // workgroup number -> kv head, head of its group, sequence, tile
     uint32_t tiles;
+    uint32_t first_wg;                                    // of this launch
     AttentionDev P;
     NarrowPost post;
 };
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const Atte
     __shared__ __attribute__((aligned(16))) int8_t lds_v[2][kKeys * VROW];
 
     AttentionTile T;
-    if (!attention_tile(A, blockIdx.x, kQueries, &T)) return;
+    if (!attention_tile(A, A.first_wg + blockIdx.x, kQueries, &T)) return;
     const int32_t nq = T.nq, nk = T.nk;
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const 
     uint32_t *lds_sum = reinterpret_cast<uint32_t *>(lds_top + 32);
 
     AttentionTile T;
-    if (!attention_tile(A, blockIdx.x, 32, &T)) return;
+    if (!attention_tile(A, A.first_wg + blockIdx.x, 32, &T)) return;
     const int32_t nq = T.nq, nk = T.nk;
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

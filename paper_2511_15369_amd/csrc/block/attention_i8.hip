@@ -1,4 +1,6 @@
 // Attention over packed prompts: the launch.
+#include <algorithm>
+
 #include "attention_i8.h"
 
 namespace iptq {
@@ -23,13 +25,19 @@ hipError_t attention_i8_dispatch(const AttentionCall &c, hipStream_t stream)
     a.tiles = ((uint32_t)c.max_q + kQueries - 1) / kQueries;
     const bool few = (int64_t)a.tiles * pairs < 256;
     if (few) a.tiles = ((uint32_t)c.max_q + 31) / 32;
-    const uint32_t grid = a.tiles * pairs;                // below 2^31: checked
-    switch (c.dim) {
-    case 32: return attention_i8_launch_32(a, few, grid, stream);
-    case 64: return attention_i8_launch_64(a, few, grid, stream);
-    case 96: return attention_i8_launch_96(a, few, grid, stream);
-    default: return attention_i8_launch_128(a, few, grid, stream);
+    const uint32_t wgs = a.tiles * pairs;                 // below 2^31: checked
+    for (a.first_wg = 0; a.first_wg < wgs; a.first_wg += kLaunchMost) {
+        const uint32_t grid = std::min(wgs - a.first_wg, kLaunchMost);
+        hipError_t e;
+        switch (c.dim) {
+        case 32: e = attention_i8_launch_32(a, few, grid, stream); break;
+        case 64: e = attention_i8_launch_64(a, few, grid, stream); break;
+        case 96: e = attention_i8_launch_96(a, few, grid, stream); break;
+        default: e = attention_i8_launch_128(a, few, grid, stream);
+        }
+        if (e != hipSuccess) return e;
     }
+    return hipSuccess;
 }
 
 }  // namespace iptq

@@ -17,6 +17,7 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 
+constexpr uint32_t kLaunchMost = 1u << 22;                // workgroups of a launch: its threads are counted in 32 bits
 constexpr int kGroup = 64;            // channels that share one step of the 4-bit cache
 
 // Unsigned division by a run-time constant (the compiler's own goes through floating point).

@@ -192,23 +192,27 @@ static void rmsnorm_launch(const RmsnormArgs &a, bool fast, hipStream_t stream)
                   dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, stream, a);
 }
 
-hipError_t rmsnorm_i32_dispatch(const RmsnormCall &c, hipStream_t stream)
+// `rows` of a call's rows, from `first` on
+static void rmsnorm_rows(const RmsnormCall &c, int64_t first, int64_t rows, hipStream_t stream)
 {
+    const int64_t at = first * c.cols;
     RmsnormArgs a;
-    a.x = c.x; a.residual = c.residual; a.residual_out = c.residual_out; a.gain = c.gain; a.out = c.out; a.row_scales = c.row_scales;
-    a.rows = (int32_t)c.rows; a.cols = c.cols; a.eps_sum = c.eps_sum; a.root_cols = c.root_cols;
+    a.x = c.x ? c.x + at : nullptr; a.residual = c.residual ? c.residual + at : nullptr;
+    a.residual_out = c.residual_out ? c.residual_out + at : nullptr; a.row_scales = c.row_scales ? c.row_scales + first : nullptr;
+    a.gain = c.gain; a.out = c.out + at;
+    a.rows = (int32_t)rows; a.cols = c.cols; a.eps_sum = c.eps_sum; a.root_cols = c.root_cols;
     a.p = c.post;
     const bool fast = c.cols >= 4 && c.in_s >= 16 && (c.post.s >= 16 || c.row_scales);
     a.in = shift_of(c.in_m, c.in_s, fast);
     a.post = shift_of(c.post.m, c.post.s, fast && c.post.s >= 16);
     if (c.cols < 4) {
-        launch_kernel(rmsnorm_narrow_kernel, dim3(((uint32_t)c.rows + 255) / 256), dim3(256), 0, stream, a);
-        return take_launch_status();
+        launch_kernel(rmsnorm_narrow_kernel, dim3(((uint32_t)rows + 255) / 256), dim3(256), 0, stream, a);
+        return;
     }
     const int chunks = (c.cols + 3) / 4;
     // Wavefronts per row: one up to 1024 values; beyond, four with up to eight chunks a lane while there are rows enough to fill the
     // chip, else as many as give a lane one or two.
-    const bool few = c.rows < 1024;
+    const bool few = rows < 1024;
     if (chunks <= 64) rmsnorm_launch<1, 1>(a, fast, stream);
     else if (chunks <= 128 && !few) rmsnorm_launch<1, 2>(a, fast, stream);
     else if (chunks <= 256 && !few) rmsnorm_launch<1, 4>(a, fast, stream);
@@ -222,6 +226,11 @@ hipError_t rmsnorm_i32_dispatch(const RmsnormCall &c, hipStream_t stream)
     else if (chunks <= 1024) rmsnorm_launch<16, 1>(a, fast, stream);
     else if (chunks <= 2048) rmsnorm_launch<16, 2>(a, fast, stream);
     else rmsnorm_launch<16, 4>(a, fast, stream);
+}
+
+hipError_t rmsnorm_i32_dispatch(const RmsnormCall &c, hipStream_t stream)
+{
+    for (int64_t r = 0; r < c.rows; r += kLaunchMost) rmsnorm_rows(c, r, std::min<int64_t>(c.rows - r, kLaunchMost), stream);
     return take_launch_status();
 }
 

@@ -84,6 +84,7 @@ extern "C" int iptq_attention_i8(const int8_t *d_q, int64_t q_stride, const int8
         if (n_seq > 0 && q_tokens / n_seq < max_q) max_q = (int32_t)(q_tokens / n_seq);
     }
     if (n_seq == 0 || max_q == 0 || q_tokens == 0) return IPTQ_OK;
+    if (max_q > q_tokens) max_q = (int32_t)q_tokens;
     const int64_t tiles = ((int64_t)max_q + 31) / 32;
     if (tiles * n_seq * heads >= ((int64_t)1 << 31)) return IPTQ_ERR_SHAPE;
     if (!d_q || !d_out || (k_tokens > 0 && (!d_k || !d_v))) return IPTQ_ERR_NULL;
@@ -136,7 +137,7 @@ extern "C" int iptq_cache_store_i4(const iptq_cache_i4_t *cache, const int8_t *d
     if (rc != IPTQ_OK) return rc;
     const int64_t kw = (int64_t)c.C.kv_heads * c.C.dim;
     if (tokens < 0 || tokens >= ((int64_t)1 << 31) || k_stride < kw || v_stride < kw || k_stride >= ((int64_t)1 << 31) ||
-        v_stride >= ((int64_t)1 << 31) || (tokens + 63) / 64 * c.C.kv_heads >= ((int64_t)1 << 31))
+        v_stride >= ((int64_t)1 << 31) || (tokens + 63) / 64 * c.C.kv_heads >= ((int64_t)1 << 24))
         return IPTQ_ERR_SHAPE;
     if (tokens == 0) return IPTQ_OK;
     if (!d_k || !d_v || !d_slots) return IPTQ_ERR_NULL;
@@ -158,7 +159,8 @@ static int plan_cache_attention(const iptq_cache_i4_t *cache, int32_t n_seq, int
     if (n_seq < 0 || q_tokens < 1 || q_tokens > IPTQ_CACHE_QUERIES_MAX || max_pages < 0 ||
         (int64_t)max_pages * c->C.page_tokens > IPTQ_CACHE_KEYS_MAX)
         return IPTQ_ERR_SHAPE;
-    if ((int64_t)n_seq * heads * q_tokens >= ((int64_t)1 << 24)) return IPTQ_ERR_SHAPE;
+    const int64_t rows = (int64_t)n_seq * heads * q_tokens, units = ((int64_t)max_pages * c->C.page_tokens + 1023) / 1024;
+    if (rows >= ((int64_t)1 << 24) || rows * units >= ((int64_t)1 << 24)) return IPTQ_ERR_SHAPE;      // (a launch's threads are counted in 32 bits)
     c->n_seq = n_seq; c->q_tokens = q_tokens; c->heads = heads; c->max_pages = max_pages;
     return IPTQ_OK;
 }

@@ -83,7 +83,8 @@ def test_a_cache_is_checked(code, change):
 @pytest.mark.parametrize("code,change", [
     (0, dict(tokens=0)), (SHAPE, dict(tokens=-1)), (SHAPE, dict(tokens=1 << 31)), (SHAPE, dict(ks=127)), (SHAPE, dict(vs=1 << 31)),
     (NULL, dict(k=None)), (NULL, dict(v=None)), (NULL, dict(slots=None)), (ALIGN, dict(slots=8 * BASE + 2)), (PARAM, dict(k=BASE)),
-    (PARAM, dict(v=4 * BASE + 639)), (PARAM, dict(slots=2 * BASE - 16)), (PARAM, dict(k=3 * BASE - 639))])
+    (PARAM, dict(v=4 * BASE + 639)), (PARAM, dict(slots=2 * BASE - 16)), (PARAM, dict(k=3 * BASE - 639)), (SHAPE, dict(tokens=1 << 29)),
+    (NULL, dict(tokens=(1 << 29) - 64, k=None))])
 def test_a_store_refuses(code, change):
     assert store(cache(), **change) == code
 
@@ -104,9 +105,21 @@ def attend(c, p=params(), **k):
     (SHAPE, dict(size=-1)), (NULL, dict(n=1, q=None)), (NULL, dict(n=1, out=None)), (NULL, dict(n=1, lengths=None)),
     (NULL, dict(n=1, pages=None)), (ALIGN, dict(n=1, pages=7 * BASE + 1)), (ALIGN, dict(n=1, lengths=8 * BASE + 2)),
     (PARAM, dict(n=1, out=6 * BASE + 511)), (PARAM, dict(n=1, out=BASE)), (PARAM, dict(n=1, out=7 * BASE + 15)),
-    (PARAM, dict(n=1, out=8 * BASE)), (PARAM, dict(n=1, out=3 * BASE + 10 * 2 * 32 * 32 - 1))])
+    (PARAM, dict(n=1, out=8 * BASE)), (PARAM, dict(n=1, out=3 * BASE + 10 * 2 * 32 * 32 - 1)), (SHAPE, dict(n=1 << 21)), (NULL, dict(n=(1 << 21) - 1, q=None)),
+    (SHAPE, dict(n=1 << 20, max_pages=33)), (NULL, dict(n=(1 << 20) - 1, max_pages=33, q=None)), (SHAPE, dict(n=1 << 14, max_pages=4096))])
 def test_cache_attention_refuses(code, change):
     assert attend(cache(), **change) == code
+
+
+@pytest.mark.parametrize("n,heads,t,max_pages", [(0, 8, 1, 4096), (0, 8, 64, 0), (1 << 20, 8, 1, 0), (65535, 2, 1, 4096), ((1 << 24) // 2 - 1, 2, 1, 3)])
+def test_cache_workspaces_at_their_ends(n, heads, t, max_pages):
+    """No sequence, no page, as many as there may be: a size that is none or fits its scores and sums."""
+    size = ctypes.c_int64(-1)
+    assert block._lib().iptq_attention_cache_i4_workspace(ctypes.byref(cache()), n, t, heads, max_pages, ctypes.byref(size)) == 0
+    keys = max_pages * 32
+    whole = n * 2 <= 1 << 22 and keys <= 1024            # (heads on two kv heads)
+    assert size.value % 16 == 0 and (size.value == 0) == (n == 0 or whole)
+    assert size.value == 0 or n * heads * t * keys * 2 < size.value < n * heads * t * (keys * 2 + 256 + 128 * 280)
 
 
 @pytest.mark.parametrize("heads,t,max_pages", [(2, 1, 4096), (128, 4, 4096), (8, 1, 3)])

@@ -570,6 +570,157 @@ def test_a_block_over_prompts_then_tokens():
         assert np.array_equal(a.cpu().numpy(), w)
 
 
+@pytest.mark.parametrize("native", [True, False])
+def test_either_binding(native, monkeypatch):
+    """The native call module and ctypes take the same arguments and make the same calls."""
+    import torch
+    b = _Block(1)
+    b.on_gpu()
+    ip.requant_rows(*[torch.zeros(s, dtype=t, device="cuda") for s, t in (((1, 8), torch.int32), (1, torch.int32), ((1, 8), torch.int8))], 1, 8, 1, 1,
+                    ip.Dyadic(1, 0, 0, -128, 127))       # (the module is bound with a process's first call)
+    if not native:
+        monkeypatch.setattr(ip.binding, "_fast", None)
+    elif ip.binding._fast is None:
+        pytest.skip("the native call module is not built")
+    n = 40
+    stream, slots = b.rng.integers(-20000, 20000, (n, b.cols)).astype(np.int32), b.rng.permutation(b.pages * b.page)[:n].astype(np.int32)
+    off = np.array([0, n], np.int32)
+    got = b.gpu(None, _cuda(stream), _cuda(slots), lambda q, k, v, o: ip.attention_i8(q, k, v, _cuda(off), _cuda(off), 1, n, o, _params(b.prompt)))
+    want = b.oracle(None, stream, slots, lambda q, k, v: ob.packed(q, k, v, off, off, n, b.prompt, np.zeros_like(q)))
+    for g, w in zip(got, want):
+        assert np.array_equal(g.cpu().numpy().reshape(w.shape), w)
+    tables, lengths = b.rng.permutation(b.pages)[None, :8].astype(np.int32), [250]
+    q = b.rng.integers(-90, 90, (1, b.heads, b.dim)).astype(np.int8)
+    o = torch.empty(q.shape, dtype=torch.int8, device="cuda")
+    ip.attention_cache_i4(_cuda(q), b.cache, _cuda(tables), _cuda(np.array(lengths, np.int32)), 1, 1, o, b.work, _params(b.decode))
+    assert np.array_equal(o.cpu().numpy(), ob.attention_cache(q, b.cache_np, tables, lengths, 1, b.decode))
+    if not native:
+        test_the_binding_refuses()
+
+
+# ----------------------------------------------------------------------------- sizes that pass 32 bits, launches of more workgroups than one may have
+def test_rows_past_32_bits():
+    """Tokens 2 MiB apart: the last rows lie behind 4 GiB."""
+    import torch
+    rng = np.random.default_rng(11)
+    n, heads, kv_heads, dim, apart = 2200, 2, 1, 64, 2 << 20
+    rows = [torch.empty(n * apart, dtype=torch.int8, device="cuda").view(n, apart) for _ in range(2)]
+    view = lambda t, at, h: t[:, at:at + h * dim].unflatten(1, (h, dim))  # noqa: E731
+    q, k, v = (rng.integers(-60, 60, (n, h, dim)).astype(np.int8) for h in (heads, kv_heads, kv_heads))
+    dq, dk, dv, out = view(rows[0], 8, heads), view(rows[0], 500, kv_heads), view(rows[0], 701, kv_heads), view(rows[1], 77, heads)
+    for d, h in ((dq, q), (dk, k), (dv, v)):
+        d.copy_(_cuda(h))
+    p = _attention(rng, dim, 1200 * dim ** 0.5, keys=n)
+    ip.attention_i8(dq, dk, dv, None, None, 1, n, out, _params(p))
+    assert np.array_equal(out.cpu().numpy(), ob.attention(q, k, v, p))
+    cache = _cache(rng, n // 16 + 1, kv_heads, 16, dim)
+    d, c = _on_gpu(cache)
+    slots = rng.permutation((n // 16 + 1) * 16)[:n].astype(np.int32)
+    ip.cache_store_i4(c, dk, dv, _cuda(slots), n)
+    for a, w in zip(d, ob.store(cache, k, v, slots)):
+        assert np.array_equal(a.cpu().numpy(), w)
+
+
+def test_a_cache_past_32_bits():
+    """Pages behind 4 GiB of codes."""
+    import torch
+    rng = np.random.default_rng(12)
+    pages, page, dim = 1 << 21, 64, 64
+    d = [torch.empty(s, dtype=torch.uint8, device="cuda") for s in ((pages, 1, page, 32), (pages, 1, page, 1), (pages, 1, 32, page), (pages, 1, page, 1))]
+    c = ip.cache_i4(*d, dim)
+    used = np.array([pages - 1, 3, pages // 2 + 1, pages - 2, 0], np.int32)
+    n = 5 * page - 7
+    k, v = (rng.integers(-90, 90, (n, 1, dim)).astype(np.int8) for _ in range(2))
+    slots = (used[np.arange(n) // page].astype(np.int64) * page + np.arange(n) % page).astype(np.int32)
+    ip.cache_store_i4(c, _cuda(k), _cuda(v), _cuda(slots), n)
+    small = ob.store([np.zeros(t.shape[1:], np.uint8)[None].repeat(5, 0) for t in d], k, v, np.arange(n, dtype=np.int32))
+    q = rng.integers(-90, 90, (1, 4, dim)).astype(np.int8)
+    for spare in (0, 200):                               # one workgroup, and several
+        p = _attention(rng, dim, _spread(dim), cache=True)
+        table = np.concatenate([used, np.full(spare, -1)]).astype(np.int32)[None]
+        out = torch.empty(q.shape, dtype=torch.int8, device="cuda")
+        size = ip.attention_cache_i4_workspace(c, 1, 1, 4, table.shape[1])
+        ip.attention_cache_i4(_cuda(q), c, _cuda(table), _cuda(np.array([n], np.int32)), 1, 1, out, torch.empty(size, dtype=torch.uint8, device="cuda"),
+                              _params(p))
+        assert np.array_equal(out.cpu().numpy(), ob.attention_cache(q, small, np.arange(5, dtype=np.int32)[None], [n], 1, p))
+
+
+def test_values_past_32_bits():
+    """Rows of the norm and of the requantization behind 2^31 values."""
+    import torch
+    rng = np.random.default_rng(13)
+    rows, cols, last = (1 << 20) + 9, 2052, 5
+    x, stream = (torch.zeros((rows, cols), dtype=torch.int32, device="cuda") for _ in range(2))
+    hx = rng.integers(-2 ** 20, 2 ** 20, (last, cols)).astype(np.int32)
+    x[-last:] = _cuda(hx)
+    gain, post = rng.integers(-2 ** 14, 2 ** 14, cols).astype(np.int16), Dyadic(20000, 29, 2, -128, 127)
+    out, scales = torch.empty((rows, cols), dtype=torch.int8, device="cuda"), torch.empty(rows, dtype=torch.int32, device="cuda")
+    ip.rmsnorm_i32(x, stream, _cuda(gain), stream, out, scales, rows, cols, ip.RmsnormParams(20000, 16, 3, _dyadic(post)))
+    want = ob.rmsnorm(hx, np.zeros_like(hx), gain, 20000, 16, 3, post, True)
+    for d, w in zip((out, stream, scales), want):
+        assert np.array_equal(d[-last:].cpu().numpy(), w) and not d[-last - 3:-last].any()
+    ip.requant_rows(x, scales, out, rows, cols, 30, 1, _dyadic(post))
+    assert np.array_equal(out[-last:].cpu().numpy(), ob.requant_rows(hx, want[2], 30, post)) and torch.all(out[:-last] == 2)
+
+
+@pytest.mark.parametrize("cols", [2, 5])
+def test_norm_of_more_rows_than_a_launch_has(cols):
+    import torch
+    rng = np.random.default_rng(cols)
+    rows, cut = (1 << 22) + 77, 1 << 21
+    x = torch.randint(-2 ** 20, 2 ** 20, (rows, cols), dtype=torch.int32, device="cuda")
+    gain, p = _cuda(rng.integers(-2 ** 14, 2 ** 14, cols).astype(np.int16)), ip.RmsnormParams(20000, 16, 3, ip.Dyadic(20000, 29, 0, -128, 127))
+    got = [torch.empty((rows, cols), dtype=torch.int8, device="cuda") for _ in range(2)]
+    scales = [torch.empty(rows, dtype=torch.int32, device="cuda") for _ in range(2)]
+    ip.rmsnorm_i32(x, None, gain, None, got[0], scales[0], rows, cols, p)
+    for a, b in ((0, cut), (cut, rows)):
+        ip.rmsnorm_i32(x[a:b], None, gain, None, got[1][a:b], scales[1][a:b], b - a, cols, p)
+    assert torch.equal(*got) and torch.equal(*scales)
+    want = ob.rmsnorm(x[-90:].cpu().numpy(), None, gain.cpu().numpy(), 20000, 16, 3, Dyadic(20000, 29, 0, -128, 127), True)
+    assert np.array_equal(got[0][-90:].cpu().numpy(), want[0])
+
+
+def test_prompts_of_more_workgroups_than_a_launch_has():
+    """65536 sequences of one token and one of 8960: tiles for the longest of each, over several launches."""
+    import torch
+    rng = np.random.default_rng(14)
+    n, long, dim = 65537, 8960, 32
+    at = np.concatenate([np.arange(n), [n - 1 + long]]).astype(np.int32)
+    tokens = int(at[-1])
+    q, k, v = (rng.integers(-60, 60, (tokens, 1, dim)).astype(np.int8) for _ in range(3))
+    p = _attention(rng, dim, 1200 * dim ** 0.5, keys=400)
+    d, d_at = [_cuda(x) for x in (q, k, v)], _cuda(at)
+    out = torch.empty((tokens, 1, dim), dtype=torch.int8, device="cuda")
+    ip.attention_i8(*d, d_at, d_at, n, long, out, _params(p))
+    apart = torch.empty_like(out)
+    ip.attention_i8(*d, d_at, d_at, n - 1, 1, apart, _params(p))
+    ip.attention_i8(*d, d_at[-2:], d_at[-2:], 1, long, apart, _params(p))
+    assert torch.equal(out, apart)
+    few = np.array([0, 1, 2, 3], np.int32)
+    assert np.array_equal(out[:3].cpu().numpy(), ob.packed(q[:3], k[:3], v[:3], few, few, 1, p, np.zeros_like(q[:3])))
+
+
+def test_short_caches_of_more_workgroups_than_a_launch_has():
+    import torch
+    rng = np.random.default_rng(15)
+    n, heads, dim = 1 << 17, 33, 32
+    cache = _cache(rng, 3, heads, 16, dim)
+    d, c = _on_gpu(cache)
+    p = _attention(rng, dim, _spread(dim), 1, 1, cache=True)
+    q = torch.randint(-90, 90, (n, heads, dim), dtype=torch.int8, device="cuda")
+    table, lengths = torch.randint(0, 3, (n, 2), dtype=torch.int32, device="cuda"), torch.randint(0, 33, (n,), dtype=torch.int32, device="cuda")
+    outs = [torch.empty_like(q) for _ in range(2)]
+    size = ip.attention_cache_i4_workspace(c, n, 1, heads, 2)
+    assert size > 0 and ip.attention_cache_i4_workspace(c, n // 2, 1, heads, 2) == 0
+    ip.attention_cache_i4(q, c, table, lengths, n, 1, outs[0], torch.empty(size, dtype=torch.uint8, device="cuda"), _params(p))
+    for a in (0, n // 2):
+        b = a + n // 2
+        ip.attention_cache_i4(q[a:b], c, table[a:b], lengths[a:b], n // 2, 1, outs[1][a:b], None, _params(p))
+    assert torch.equal(*outs)
+    want = ob.attention_cache(q[-9:].cpu().numpy(), cache, table[-9:].cpu().numpy(), lengths[-9:].cpu().numpy(), 1, p)
+    assert np.array_equal(outs[0][-9:].cpu().numpy(), want)
+
+
 def test_calls_go_to_the_current_stream():
     """Two streams at once, each with its own workspace: every call waits for what its stream wrote before."""
     import torch
