@@ -390,7 +390,7 @@ typedef struct {
  * Stores `tokens` rows of keys and values (int8, as in iptq_attention_i8) into the cache: row i goes to
  * slot d_slots[i] = page * page_tokens + position (int32, device).  A slot outside [0, n_pages * page_tokens) is skipped
  * (padding: -1).  No two rows of a call may name the same slot (what that slot then holds is not
- * specified; nothing else is touched).  tokens / 64 (rounded up) * kv_heads < 2^24.
+ * specified; nothing else is touched).  tokens / 16 (rounded up) * kv_heads < 2^24.
  */
 int iptq_cache_store_i4(const iptq_cache_i4_t *cache /*host*/, const int8_t *d_k, int64_t k_stride, const int8_t *d_v, int64_t v_stride,
                         const int32_t *d_slots, int64_t tokens, void *stream);

@@ -137,7 +137,7 @@ extern "C" int iptq_cache_store_i4(const iptq_cache_i4_t *cache, const int8_t *d
     if (rc != IPTQ_OK) return rc;
     const int64_t kw = (int64_t)c.C.kv_heads * c.C.dim;
     if (tokens < 0 || tokens >= ((int64_t)1 << 31) || k_stride < kw || v_stride < kw || k_stride >= ((int64_t)1 << 31) ||
-        v_stride >= ((int64_t)1 << 31) || (tokens + 63) / 64 * c.C.kv_heads >= ((int64_t)1 << 24))
+        v_stride >= ((int64_t)1 << 31) || (tokens + 15) / 16 * c.C.kv_heads >= ((int64_t)1 << 24))
         return IPTQ_ERR_SHAPE;
     if (tokens == 0) return IPTQ_OK;
     if (!d_k || !d_v || !d_slots) return IPTQ_ERR_NULL;

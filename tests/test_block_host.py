@@ -83,8 +83,8 @@ def test_a_cache_is_checked(code, change):
 @pytest.mark.parametrize("code,change", [
     (0, dict(tokens=0)), (SHAPE, dict(tokens=-1)), (SHAPE, dict(tokens=1 << 31)), (SHAPE, dict(ks=127)), (SHAPE, dict(vs=1 << 31)),
     (NULL, dict(k=None)), (NULL, dict(v=None)), (NULL, dict(slots=None)), (ALIGN, dict(slots=8 * BASE + 2)), (PARAM, dict(k=BASE)),
-    (PARAM, dict(v=4 * BASE + 639)), (PARAM, dict(slots=2 * BASE - 16)), (PARAM, dict(k=3 * BASE - 639)), (SHAPE, dict(tokens=1 << 29)),
-    (NULL, dict(tokens=(1 << 29) - 64, k=None))])
+    (PARAM, dict(v=4 * BASE + 639)), (PARAM, dict(slots=2 * BASE - 16)), (PARAM, dict(k=3 * BASE - 639)), (SHAPE, dict(tokens=1 << 27)),
+    (NULL, dict(tokens=(1 << 27) - 16, k=None))])
 def test_a_store_refuses(code, change):
     assert store(cache(), **change) == code
 
