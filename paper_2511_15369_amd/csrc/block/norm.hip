@@ -1,6 +1,7 @@
 // Root-mean-square norm with the residual's addition, and requantization by row scales.
 //
 // Both are bound by HBM: 13 bytes per value of the norm (product, residual, its new value, code), 5 of the requantization.
+// 8192 rows of 5120 take 97 us (5.6 TB/s), 8192 of 6144 requantized 40.5 us (6.2 TB/s); 64 rows, 4.5 and 3.8 us, are the launch.
 // A row stays in the registers of the wavefronts that hold it, so every byte crosses once.  Rows are read in chunks of four
 // values at their natural alignment; where four does not divide a row its last chunk ends with it and starts
 // earlier, and the values it shares with the chunk before count once.
@@ -210,22 +211,23 @@ static void rmsnorm_rows(const RmsnormCall &c, int64_t first, int64_t rows, hipS
         return;
     }
     const int chunks = (c.cols + 3) / 4;
-    // Wavefronts per row: one up to 1024 values; beyond, four with up to eight chunks a lane while there are rows enough to fill the
-    // chip, else as many as give a lane one or two.
-    const bool few = rows < 1024;
+    // A row has as few wavefronts as hold it: one up to 512 values, four up to 8192, eight beyond, with the chunks a lane
+    // that its length needs (12288 values in the eight of 16384: 67 us in place of 51 for 2000 rows).  Sixteen wavefronts with fewer chunks
+    // each took longer whatever the number of rows: 1 x 4096 4.7 in place of 3.9 us, 1000 x 4096 14.6 and 10.2, as did two
+    // (1 x 2048 3.7 and 3.2).  Rows of 513 to 1024 values: four wavefronts and one chunk each where latency counts (200 x 768 3.4, one wavefront
+    // 4.0 us), one from 512 rows on (1000 x 768 4.4 and 4.8, 8192 x 768 15.5 and 19.1).
     if (chunks <= 64) rmsnorm_launch<1, 1>(a, fast, stream);
-    else if (chunks <= 128 && !few) rmsnorm_launch<1, 2>(a, fast, stream);
-    else if (chunks <= 256 && !few) rmsnorm_launch<1, 4>(a, fast, stream);
+    else if (chunks <= 128) rmsnorm_launch<1, 2>(a, fast, stream);
+    else if (chunks <= 256 && rows >= 512) rmsnorm_launch<1, 4>(a, fast, stream);
     else if (chunks <= 256) rmsnorm_launch<4, 1>(a, fast, stream);
-    else if (chunks <= 512 && !few) rmsnorm_launch<4, 2>(a, fast, stream);
-    else if (chunks <= 768 && !few) rmsnorm_launch<4, 3>(a, fast, stream);
-    else if (chunks <= 1024 && !few) rmsnorm_launch<4, 4>(a, fast, stream);
-    else if (chunks <= 1280 && !few) rmsnorm_launch<4, 5>(a, fast, stream);
-    else if (chunks <= 1536 && !few) rmsnorm_launch<4, 6>(a, fast, stream);
-    else if (chunks <= 2048 && !few) rmsnorm_launch<4, 8>(a, fast, stream);
-    else if (chunks <= 1024) rmsnorm_launch<16, 1>(a, fast, stream);
-    else if (chunks <= 2048) rmsnorm_launch<16, 2>(a, fast, stream);
-    else rmsnorm_launch<16, 4>(a, fast, stream);
+    else if (chunks <= 512) rmsnorm_launch<4, 2>(a, fast, stream);
+    else if (chunks <= 768) rmsnorm_launch<4, 3>(a, fast, stream);
+    else if (chunks <= 1024) rmsnorm_launch<4, 4>(a, fast, stream);
+    else if (chunks <= 1280) rmsnorm_launch<4, 5>(a, fast, stream);
+    else if (chunks <= 1536) rmsnorm_launch<4, 6>(a, fast, stream);
+    else if (chunks <= 2048) rmsnorm_launch<4, 8>(a, fast, stream);
+    else if (chunks <= 3072) rmsnorm_launch<8, 6>(a, fast, stream);
+    else rmsnorm_launch<8, 8>(a, fast, stream);
 }
 
 hipError_t rmsnorm_i32_dispatch(const RmsnormCall &c, hipStream_t stream)
