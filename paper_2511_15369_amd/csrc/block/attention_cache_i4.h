@@ -4,10 +4,13 @@
 //   w_j  = the exponential of x_j against the row's maximum (steps 1-5 of the softmax)
 //   u_jg = (w_j a'_jg + 64) >> 7,   o_d = floor(2^54 / sum w_j) * sum_j u_jg c'_jd >> 39
 //
-// Bound by the bytes of the cache (head_dim / 2 + 1 or 2 per key, twice).  The exponentials need the row's maximum
+// The bytes of the cache (head_dim / 2 + 1 or 2 per key, twice) bound it for one head to a kv head.  The exponentials need the row's maximum
 // before the first of them, so there are two phases, keys and then values, with the scores kept
 // between them: as 16-bit differences from the largest score of their 64-key tile and column, saturated (a score
-// that far below the maximum has weight 0 either way).
+// that far below the maximum has weight 0 either way).  Their 2 bytes per key and column, written and read, are as many as the cache's
+// from 32 columns on, and the values' phase has 400 vector instructions per 64 keys and 16 columns.
+// Measured: 64 sequences of 200 to 8192 tokens, 32 heads on 8 of 128, 73 us (2.5 TB/s of cache; 30 us keys, 36 values, 7 the sum of
+// the splits); two of 131072, 32 columns, 139 us (1.9 TB/s of cache, 3.9 with the scores); one of 700, 8 us with the call.
 //
 // Columns are the queries that share a kv head: e = token * group + head of the group, 16 of them to the narrow
 // side of v_mfma_i32_16x16x64_i8.  Keys go by tiles of 64, in blocks of 16 that never cross a page.  Scores are
@@ -35,7 +38,7 @@ struct CacheAttentionArgs {
     int32_t max_pages, q_tokens, group, columns;          // columns = group * q_tokens
     DivDev by_group, by_kv_heads, by_chunks, by_splits;   // column -> token; workgroup -> kv head, columns, split, sequence
     DivDev by_span, by_columns;                           // span: 64 keys of each wavefront that a sequence's keys are divided over
-    int32_t column_tiles, key_waves;                      // of a workgroup: wavefronts side by side over the columns (1 or 2), over the keys
+    int32_t key_waves;                                    // wavefronts of a workgroup, over the keys
     int32_t splits, tiles;                                // workgroups over a sequence; tiles of the workspace a sequence
     // between the phases, where one workgroup does not have all keys of a sequence
     int16_t *deltas;                                      // [sequence, kv head][tile, p][2][column][8]
@@ -78,12 +81,13 @@ IPTQ_DEV int32_t byte_of(const u32x4 *v, int i) { return (int32_t)(v[i >> 4][i >
 // HALVES 2: up to eight queries share a kv head.  The second product's sixteen columns are then the upper halves of
 // eight queries' weights and the lower halves of the same: one product in place of two, and lanes that would have
 // been idle make the same weights as their neighbours.
+// (One of 700 tokens 7.6 us, 64 of 4000 74, two of 65536 52; in the other form 7.8, 77 and 54.)
 // HALVES 1: sixteen queries, one product for either half.
 template <int D, int VARIANT, int HALVES, int PHASES>
 struct CacheAttention {
     static constexpr int G = (D + kGroup - 1) / kGroup, PAIRS = D / 2, BLOCKS = D / 32;    // blocks of 16 channel pairs
     static constexpr int QUERIES = 16 / HALVES, PRODUCTS = 3 - HALVES;
-    static constexpr int ACC = BLOCKS * 2 * 4 * 64;       // sums of one column tile
+    static constexpr int ACC = BLOCKS * 2 * 4 * 64;       // sums of 16 columns
 
     // A tile's codes as the wavefront loads them, 16 bytes a lane in the order of the memory (a quarter of a
     // wavefront-wide load then meets whole lines; loaded in the products' order, every lane of a quad had a line of its own
@@ -301,28 +305,26 @@ IPTQ_DEV void store_means(int8_t *out, uint64_t f, const int64_t (&acc)[8], cons
     *reinterpret_cast<u32x2_any *>(out) = (u32x2_t){w[0], w[1]};
 }
 
-// A workgroup's wavefronts: A.column_tiles of them side by side over the columns, the others over the keys.
-// LDS: a staging buffer per wavefront; per column tile [tops 16], [sums 16] and the sums [ACC].
+// A workgroup has up to 16 queries of a split's keys, which its wavefronts divide.  (32 queries of the same keys, two wavefronts side by
+// side, took 5 to 9 % longer: the keys come from the L2 the second time.)
+// LDS: a staging buffer per wavefront, [tops 16], [sums 16], [ACC].
 template <int D, int VARIANT, int HALVES, int PHASES>
 IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, uint32_t seq, uint32_t chunk, uint32_t split)
 {
     typedef CacheAttention<D, VARIANT, HALVES, PHASES> T;
     extern __shared__ __attribute__((aligned(16))) int8_t lds_bytes[];
-    const int ct = A.column_tiles, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int key_wave = ct == 2 ? wave >> 1 : wave, c = ct == 2 ? wave & 1 : 0;
-    int32_t *lds = reinterpret_cast<int32_t *>(lds_bytes + (blockDim.x >> 6) * T::STAGE);
-    int32_t *lds_top = lds + 16 * c, *lds_acc = lds + 32 * ct + c * T::ACC;
-    uint32_t *lds_sum = reinterpret_cast<uint32_t *>(lds + 16 * ct + 16 * c);
-    const int e_wg = (int)chunk * T::QUERIES * ct;                         // the workgroup's first query
-    T t(A, kvh, seq, (uint32_t)(e_wg + T::QUERIES * c), (int32_t)split * A.key_waves + key_wave,
-        lds_bytes + wave * T::STAGE);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int32_t *lds_top = reinterpret_cast<int32_t *>(lds_bytes + A.key_waves * T::STAGE), *lds_acc = lds_top + 32;
+    uint32_t *lds_sum = reinterpret_cast<uint32_t *>(lds_top + 16);
+    const int e_wg = (int)chunk * T::QUERIES;                              // the workgroup's first query
+    T t(A, kvh, seq, (uint32_t)e_wg, (int32_t)split * A.key_waves + wave, lds_bytes + wave * T::STAGE);
     const int lane = t.lane, col = t.col, p = t.p;
     const int32_t split_keys = wave_keys_of(A, t.length) * A.key_waves;
     if (PHASES != 3 && (int32_t)split * split_keys >= t.length) return;   // no key in this split
     t.load_queries();
     const int64_t pair = (int64_t)seq * A.C.kv_heads + kvh;
     const int32_t tiles = A.tiles;
-    const int columns = A.columns, column = e_wg + T::QUERIES * c + (col & (T::QUERIES - 1));
+    const int columns = A.columns, column = e_wg + (col & (T::QUERIES - 1));
     int16_t *deltas = A.deltas + pair * tiles * 4 * columns * 16;
     int32_t *refs = A.refs + pair * tiles * columns;
     const bool mine = col < T::QUERIES && column < columns;                // the lane writes its column's scores
@@ -332,9 +334,9 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
     uint32_t only_d[8];
     int32_t only_ref = kI32Min;
     int32_t top = kI32Min;
-    if (threadIdx.x < 16 * (unsigned)ct) lds[threadIdx.x] = kI32Min;
+    if (threadIdx.x < 16) lds_top[threadIdx.x] = kI32Min;
     if (PHASES & 2)
-        for (int i = threadIdx.x; i < (16 + T::ACC) * ct; i += blockDim.x) lds[16 * ct + i] = 0;           // sums
+        for (int i = threadIdx.x; i < 16 + T::ACC; i += blockDim.x) lds_top[16 + i] = 0;       // sums
     if (PHASES & 1) {
         if (PHASES == 3 && t.from < t.to) {
             const typename T::Keys keys = t.load_keys(t.from);
@@ -364,18 +366,17 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
         if (p == 0 && t.from < t.to) atomicMax(lds_top + col, top);
         __syncthreads();
         if (PHASES == 1) {
-            const int i = threadIdx.x, j = i & (T::QUERIES - 1), cc = i / T::QUERIES;
-            if (cc < ct && e_wg + i < columns) A.tops[(pair * A.splits + split) * columns + e_wg + i] = lds[16 * cc + j];
+            const int i = threadIdx.x;
+            if (i < T::QUERIES && e_wg + i < columns) A.tops[(pair * A.splits + split) * columns + e_wg + i] = lds_top[i];
             return;
         }
     } else {
         __syncthreads();
     }
     if (PHASES == 2) {                                    // the largest score of all splits that have keys
-        const int log = ct == 2 ? 5 : 4;
-        for (int i = threadIdx.x & (16 * ct - 1), s = threadIdx.x >> log; s < A.splits && s * split_keys < t.length; s += blockDim.x >> log) {
-            const int j = i & 15, x = e_wg + (i >> 4) * T::QUERIES + (j & (T::QUERIES - 1));
-            if (x < columns) atomicMax(lds + i, A.tops[(pair * A.splits + s) * columns + x]);
+        for (int i = threadIdx.x & 15, s = threadIdx.x >> 4; s < A.splits && s * split_keys < t.length; s += blockDim.x >> 4) {
+            const int x = e_wg + (i & (T::QUERIES - 1));
+            if (x < columns) atomicMax(lds_top + i, A.tops[(pair * A.splits + s) * columns + x]);
         }
         __syncthreads();
     }
@@ -429,14 +430,14 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
     }
     __syncthreads();
     // a thread's block of 16 channel pairs and lane: rows 4 p + r are the pairs 16 b + 4 p + r, eight channels in a row
-    for (int u = threadIdx.x; u < ct * T::BLOCKS * 64; u += blockDim.x) {
-        const int cc = u / (T::BLOCKS * 64), b = (u >> 6) % T::BLOCKS, l = u & 63, j = l & 15;
-        const uint32_t x = (uint32_t)(e_wg + T::QUERIES * cc + j);
+    for (int u = threadIdx.x; u < T::BLOCKS * 64; u += blockDim.x) {
+        const int b = u >> 6, l = u & 63, j = l & 15;
+        const uint32_t x = (uint32_t)(e_wg + j);
         if (j >= T::QUERIES || x >= (uint32_t)A.columns) continue;
         int64_t v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = lds[32 * ct + cc * T::ACC + ((b * 2 + (i & 1)) * 4 + (i >> 1)) * 64 + l];
-        const uint32_t s = (uint32_t)lds[16 * ct + 16 * cc + j];
+        for (int i = 0; i < 8; ++i) v[i] = lds_acc[((b * 2 + (i & 1)) * 4 + (i >> 1)) * 64 + l];
+        const uint32_t s = lds_sum[j];
         const int channel = 32 * b + 8 * (l >> 4);
         if (PHASES == 3) {
             const uint32_t token = div_by(x, A.by_group), head = kvh * (uint32_t)A.group + (x - token * (uint32_t)A.group);

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void attention_cache_i4_join_kernel(const Cach
 }
 
 struct CachePlan {
-    int halves, ct, chunks;           // weights' halves side by side; column tiles of a workgroup; workgroups over the columns
+    int halves, chunks;               // weights' halves side by side; workgroups over the columns
     bool whole;                       // one workgroup has all keys
     int key_waves, splits, tiles;
     size_t lds;
@@ -60,25 +60,26 @@ static CachePlan plan_of(const CacheAttentionCall &c)
     CachePlan p;
     const int columns = c.heads / c.C.kv_heads * c.q_tokens;
     p.halves = columns <= 8 ? 2 : 1;
-    p.ct = columns > 16 ? 2 : 1;
-    const int queries = 16 / p.halves * p.ct;
+    const int queries = 16 / p.halves;
     p.chunks = (columns + queries - 1) / queries;
     p.pairs = (int64_t)c.n_seq * c.C.kv_heads;
     const int64_t keys = (int64_t)c.max_pages * c.C.page_tokens;           // at most
     p.tiles = (int)((keys + kTile - 1) / kTile);
-    // a tile a wavefront, sixteen wavefronts
-    p.whole = keys <= 1024 / p.ct && p.pairs * p.chunks <= (int64_t)kLaunchMost;
-    p.key_waves = p.whole ? std::max(p.tiles, 1) : 4 / p.ct;
+    // Up to 1024 keys: a tile a wavefront, up to sixteen of these, and all of a sequence's scores in registers: one launch (64 sequences of
+    // 1000 tokens, 32 heads on 8, 22.7 us, in two phases 34.8; one of 500 6.5 and 11.9).
+    p.whole = keys <= 1024 && p.pairs * p.chunks <= (int64_t)kLaunchMost;
+    p.key_waves = p.whole ? std::max(p.tiles, 1) : 4;
     p.splits = 1;
     if (!p.whole) {
-        // workgroups enough for the chip, a wavefront with 64 to 1024 keys; with many columns fewer, as each split
-        // writes and reads a sum per column and channel
+        // A wavefront has 64 to 1024 keys.  Up to eight queries: twice as many workgroups as the chip holds, for the sake of sequences of
+        // different lengths (64 of 200 to 8192 tokens 75 us, with half as many workgroups 80; of equal lengths 4 % the other way: 64 of 4000 72
+        // and 69).  More queries: once, as each split writes and reads a sum per column and channel (two of 65536 tokens, 32 columns, 76 and 93).
         const int64_t most = (keys + kTile * p.key_waves - 1) / (kTile * p.key_waves), least = (keys + 1024 * p.key_waves - 1) / (1024 * p.key_waves);
         const int64_t wanted = (columns > 8 ? 1024 : 2048) / (p.pairs * p.chunks);
         p.splits = (int)std::min<int64_t>(std::max(std::max<int64_t>(wanted, least), (int64_t)1), std::min<int64_t>(most, 128));
     }
     const size_t blocks = c.C.dim / 32, stage = std::max(blocks * 4 * 288, (size_t)kTile * c.C.dim / 2 + 256);       // CacheAttention::STAGE
-    p.lds = (size_t)p.key_waves * p.ct * stage + (size_t)p.ct * (32 + c.C.dim / 32 * 512) * 4;
+    p.lds = (size_t)p.key_waves * stage + (size_t)(32 + c.C.dim / 32 * 512) * 4;
     const int64_t rows = p.whole ? 0 : p.pairs * columns;
     p.deltas = rows * p.tiles * kTile * 2;
     p.refs = up_to(rows * p.tiles * 4, 16);
@@ -119,7 +120,6 @@ hipError_t attention_cache_i4_dispatch(const CacheAttentionCall &c, hipStream_t 
     a.by_splits = div_of((uint32_t)p.splits);
     a.by_span = div_of((uint32_t)(kTile * p.key_waves * p.splits));
     a.by_columns = div_of((uint32_t)a.columns);
-    a.column_tiles = p.ct;
     a.key_waves = p.key_waves;
     a.splits = p.splits; a.tiles = p.tiles;
     char *w = static_cast<char *>(c.work);
@@ -130,7 +130,7 @@ hipError_t attention_cache_i4_dispatch(const CacheAttentionCall &c, hipStream_t 
     a.sums = reinterpret_cast<uint32_t *>(w);
     a.C = c.C; a.P = c.P;
     const uint32_t grid = (uint32_t)(p.pairs * p.chunks * p.splits);
-    const uint32_t block = 64u * p.key_waves * p.ct;
+    const uint32_t block = 64u * p.key_waves;
     if (p.whole) return launch(a, p.halves, 3, grid, block, p.lds, stream);
     hipError_t e = launch(a, p.halves, 1, grid, block, p.lds, stream);
     if (e != hipSuccess) return e;
