@@ -1,4 +1,4 @@
-// Attention over packed prompts: the launch.
+// Attention over packed prompts: the launches.
 #include <algorithm>
 
 #include "attention_i8.h"
@@ -20,7 +20,8 @@ hipError_t attention_i8_dispatch(const AttentionCall &c, hipStream_t stream)
     a.P = c.P;
     a.post = narrow_post_of(c.P.post.m, c.P.post.s);
     // Workgroups of 128 queries, or of 32 with their keys divided over the wavefronts where the former do not reach every
-    // compute unit.
+    // compute unit: 197 tokens of 3 heads 6.0 us (128 queries: 9.5), 512 of 32 heads 20.1 (21.1), 4000 of 4 heads 55 (116), 8000 of 4
+    // heads, 252 workgroups, 178 (229); from 256 on the other way, 900 of 32 heads 44 (32), 2000 129 (65), 64 images of 49 9.1 (6.0).
     const uint32_t pairs = (uint32_t)c.n_seq * (uint32_t)c.heads;
     a.tiles = ((uint32_t)c.max_q + kQueries - 1) / kQueries;
     const bool few = (int64_t)a.tiles * pairs < 256;
