@@ -39,6 +39,7 @@ struct CacheAttentionArgs {
     DivDev by_group, by_kv_heads, by_chunks, by_splits;   // column -> token; workgroup -> kv head, columns, split, sequence
     DivDev by_span, by_columns;                           // span: 64 keys of each wavefront that a sequence's keys are divided over
     int32_t key_waves;                                    // wavefronts of a workgroup, over the keys
+    uint32_t all_columns;                                 // of all sequences and kv heads
     int32_t splits, tiles;                                // workgroups over a sequence; tiles of the workspace a sequence
     // between the phases, where one workgroup does not have all keys of a sequence
     int16_t *deltas;                                      // [sequence, kv head][tile, p][2][column][8]
