@@ -141,20 +141,14 @@ IPTQ_DEV i32x4 values_of_block(const int8_t *src)
 
 // floor(2^54 / sum) times four sums, 46 bits down, requantized.  NARROW: the sum of the weights is below 2^24, that of the weighted
 // values below 2^31 then, and f = 2^32 fh + fl with a signed fl has two products in place of five.
-template <bool NARROW>
-IPTQ_DEV int32_t means_of(uint64_t f, const int32_t (&hi)[4], const int32_t (&lo)[4], const AttentionArgs &A)
+template <bool NARROW, typename Sum>
+IPTQ_DEV int32_t means_of(uint64_t f, const Sum (&acc)[4], const AttentionArgs &A)
 {
     const int32_t fl = (int32_t)f, fh = (int32_t)((int64_t)(f - (uint64_t)(int64_t)fl) >> 32);
     int32_t c[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        int32_t o;
-        if (NARROW) {
-            const int32_t acc = (hi[i] << 8) + lo[i];
-            o = (fh * acc + __mulhi(fl, acc)) >> 14;
-        } else {
-            o = mean_of(f, (int64_t)hi[i] * 256 + lo[i], 46);
-        }
+        const int32_t o = NARROW ? (fh * (int32_t)acc[i] + __mulhi(fl, (int32_t)acc[i])) >> 14 : mean_of(f, acc[i], 46);
         c[i] = clamp_i32(((__mul24(o, A.post.m) + A.post.rnd) >> A.post.s) + A.P.post.zp, A.P.post.qmin, A.P.post.qmax);
     }
     return (int32_t)four_bytes(c);
@@ -165,8 +159,10 @@ IPTQ_DEV void store_block(int8_t *out, uint64_t f, const i32x16 &hi, const i32x1
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int32_t h[4] = {hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]}, l[4] = {lo[4 * i], lo[4 * i + 1], lo[4 * i + 2], lo[4 * i + 3]};
-        *reinterpret_cast<i32_a1 *>(out + 8 * i + 4 * half) = means_of<NARROW>(f, h, l, A);
+        int64_t acc[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = NARROW ? (hi[4 * i + j] << 8) + lo[4 * i + j] : (int64_t)hi[4 * i + j] * 256 + lo[4 * i + j];
+        *reinterpret_cast<i32_a1 *>(out + 8 * i + 4 * half) = means_of<NARROW>(f, acc, A);
     }
 }
 
@@ -342,10 +338,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const Atte
 // heads of 64, 21 workgroups of one block per wavefront, take 6.1 us, and a launch that does nothing about 2.3.
 constexpr int kFewWaves = 8;
 
+// The wavefronts' tiles, and in the same place their sums of weighted values at the end; the maxima, the sums of the weights.
 template <int D> struct FewLds {
     static constexpr int KROW = D + 16, VROW = ValueRow<D>::bytes, stage = 32 * (KROW + VROW);      // of a wavefront
-    static constexpr int acc = D / 32 * 16 * 64 * 4;      // of either half of the weights
-    static constexpr size_t bytes = kFewWaves * stage + 2 * acc + 256;
+    static constexpr int units = D / 32 * 4 * 64, acc = units * 16;       // a wavefront's sums, four to a unit
+    static constexpr int shared = kFewWaves * (acc > stage ? acc : stage);
+    static constexpr size_t bytes = shared + 32 * 4 * (1 + kFewWaves);
 };
 
 template <int D, int VARIANT>
@@ -354,7 +352,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const 
     typedef FewLds<D> L;
     constexpr int STEPS = D / 32, KROW = L::KROW, VROW = L::VROW;
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
-    int32_t *lds_hi = reinterpret_cast<int32_t *>(lds + kFewWaves * L::stage), *lds_lo = lds_hi + L::acc / 4, *lds_top = lds_lo + L::acc / 4;
+    i32x4 *lds_acc = reinterpret_cast<i32x4 *>(lds);
+    int32_t *lds_top = reinterpret_cast<int32_t *>(lds + L::shared);
     uint32_t *lds_sum = reinterpret_cast<uint32_t *>(lds_top + 32);
 
     AttentionTile T;
@@ -403,11 +402,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const 
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const i32x4_a1 *>(p + 32 * s);
     }
-    for (int i = threadIdx.x; i < 2 * L::acc / 4; i += 64 * kFewWaves) lds_hi[i] = 0;
-    if (threadIdx.x < 32) {
-        lds_top[threadIdx.x] = kI32Min;
-        lds_sum[threadIdx.x] = 0;
-    }
+    if (threadIdx.x < 32) lds_top[threadIdx.x] = kI32Min;
     __syncthreads();
     auto scores = [&]() {
         i32x16 x = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
@@ -431,12 +426,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const 
     if (busy && half == 0) atomicMax(lds_top + col, top);
     __syncthreads();
     const int32_t start = score_start(lds_top[col], A.P.shift);
+    i32x16 acc_hi[STEPS], acc_lo[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc_hi[s][i] = acc_lo[s][i] = 0;
     if (busy) {
-        i32x16 acc_hi[STEPS], acc_lo[STEPS];
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc_hi[s][i] = acc_lo[s][i] = 0;
         uint32_t sum = 0;
         const int v_lane = (16 * half + (lane >> 1 & 7)) * VROW + 16 * (lane >> 4 & 1) + 8 * (lane & 1);
         const bool once = from + step >= most;            // its only block's scores are still there
@@ -463,36 +458,76 @@ __global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const 
             }
         }
         sum += (uint32_t)__shfl_xor((int32_t)sum, 32);
-        if (half == 0) atomicAdd(lds_sum + col, sum);
-        // 256 hi + lo of up to 508 keys fits 32 bits
-        const bool narrow = most <= 508;
+        if (half == 0) lds_sum[32 * wave + col] = sum;
+    }
+    if (most <= 0 && threadIdx.x < 32) lds_sum[threadIdx.x] = 0;
+    // The wavefronts' sums, joined by whoever makes the outputs: 256 hi + lo at once where it fits 32 bits (up to 508 keys; a wavefront's of
+    // up to 508 of its own, added up in 64), else one half after the other.
+    const int waves = max(min(kFewWaves, (most + 31) >> 5), 1);       // (without keys the first's zeros)
+    constexpr int MINE = (L::units + 64 * kFewWaves - 1) / (64 * kFewWaves);
+    auto join = [&](auto &total, bool whole) {
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
+        for (int m = 0; m < MINE; ++m)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if (narrow) {
-                    atomicAdd(lds_lo + (16 * s + i) * 64 + lane, acc_hi[s][i] * 256 + acc_lo[s][i]);
-                } else {
-                    atomicAdd(lds_hi + (16 * s + i) * 64 + lane, acc_hi[s][i]);
-                    atomicAdd(lds_lo + (16 * s + i) * 64 + lane, acc_lo[s][i]);
+            for (int j = 0; j < 4; ++j) total[m][j] = 0;
+        for (int part = whole ? 1 : 0; part < 2; ++part) {
+            __syncthreads();
+            if (wave < waves) {
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        i32x4 v;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int32_t h = acc_hi[s][4 * i + j], l = acc_lo[s][4 * i + j];
+                            v[j] = whole ? (h << 8) + l : part == 0 ? h : l;
+                        }
+                        lds_acc[wave * L::units + (4 * s + i) * 64 + lane] = v;
+                    }
+            }
+            __syncthreads();
+            const int up = part == 0 ? 8 : 0;
+#pragma unroll
+            for (int m = 0; m < MINE; ++m) {
+                const int u = threadIdx.x + 64 * kFewWaves * m;
+                if (u >= L::units) break;
+#pragma unroll
+                for (int w = 0; w < kFewWaves; ++w) {
+                    if (w >= waves) break;
+                    const i32x4 v = lds_acc[w * L::units + u];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) total[m][j] += sizeof(total[m][j]) == 4 ? v[j] : (int64_t)v[j] << up;
                 }
             }
-    }
-    __syncthreads();
-    // a thread's query and four channels: 32 s + 8 i + 4 h
-    for (int u = threadIdx.x; u < 32 * STEPS * 8; u += 64 * kFewWaves) {
-        const int q = u & 31, h = u >> 5 & 1, i = u >> 6 & 3, s = u >> 8;
-        if (T.first + q >= nq) continue;
-        const uint64_t f = floor_div_u64((uint64_t)1 << 54, lds_sum[q]);
-        int32_t hi[4], lo[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int at = (16 * s + 4 * i + j) * 64 + 32 * h + q;
-            hi[j] = lds_hi[at];
-            lo[j] = lds_lo[at];
         }
-        *reinterpret_cast<i32_a1 *>(A.out + (int64_t)(T.q0 + T.first + q) * A.out_stride + T.head * D + 32 * s + 8 * i + 4 * h) =
-            most <= 508 ? means_of<true>(f, hi, lo, A) : means_of<false>(f, hi, lo, A);
+    };
+    // a thread's query and four channels: 32 s + 8 i + 4 h
+    const int q = threadIdx.x & 31, h = threadIdx.x >> 5 & 1;
+    auto mean_factor = [&]() {
+        uint32_t sum = 0;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) sum += w < waves ? lds_sum[32 * w + q] : 0;
+        return floor_div_u64((uint64_t)1 << 54, sum);
+    };
+    auto store = [&](int m, int32_t bytes) {
+        const int u = threadIdx.x + 64 * kFewWaves * m, i = u >> 6 & 3, s = u >> 8;
+        if (u < L::units) *reinterpret_cast<i32_a1 *>(A.out + (int64_t)(T.q0 + T.first + q) * A.out_stride + T.head * D + 32 * s + 8 * i + 4 * h) = bytes;
+    };
+    if (most <= 508) {
+        int32_t total[MINE][4];
+        join(total, true);
+        if (T.first + q >= nq) return;
+        const uint64_t f = mean_factor();
+#pragma unroll
+        for (int m = 0; m < MINE; ++m) store(m, means_of<true>(f, total[m], A));
+    } else {
+        int64_t total[MINE][4];
+        join(total, most <= 15 * step);
+        if (T.first + q >= nq) return;
+        const uint64_t f = mean_factor();
+#pragma unroll
+        for (int m = 0; m < MINE; ++m) store(m, means_of<false>(f, total[m], A));
     }
 }
 
