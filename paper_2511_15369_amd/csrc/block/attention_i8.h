@@ -364,6 +364,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const 
     const int32_t row = T.first + col;
     const int32_t limit = A.P.causal ? min(max(row + T.diag + 1, 0), nk) : nk;
     const int32_t most = A.P.causal ? min(max(min(T.first + 32, nq) + T.diag, 0), nk) : nk;        // that any row sees
+    const int32_t least = A.P.causal ? min(max(T.first + T.diag + 1, 0), nk) : nk;                 // that every row sees
     int8_t *stage_k = lds + wave * L::stage, *stage_v = stage_k + 32 * KROW;
 
     const int8_t *kp = A.k + (int64_t)T.k0 * A.k_stride + T.kvh * D, *vp = A.v + (int64_t)T.k0 * A.v_stride + T.kvh * D;
@@ -419,8 +420,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const 
         if (at + step < most) load(kp, A.k_stride, at + step, kr);
         wave_lds_fence();
         x = scores();
+        if (at + 32 <= least) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) top = at + 16 * half + i < limit ? max(top, x[i]) : top;
+            for (int i = 0; i < 16; ++i) top = max(top, x[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = at + 16 * half + i < limit ? max(top, x[i]) : top;
+        }
     }
     top = max(top, __shfl_xor(top, 32));
     if (busy && half == 0) atomicMax(lds_top + col, top);
@@ -447,7 +453,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const 
             wave_lds_fence();
             if (!once) x = scores();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = at + 16 * half + i < limit ? x[i] + start : kI32Min;
+            for (int i = 0; i < 16; ++i) x[i] += start;
+            if (at + 32 > least) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = at + 16 * half + i < limit ? x[i] : kI32Min;
+            }
             i32x4 hi, lo;
             weights_of_scores<VARIANT>(x, A.P, &hi, &lo, &sum);
 #pragma unroll
