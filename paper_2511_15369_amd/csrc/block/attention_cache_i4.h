@@ -80,8 +80,8 @@ IPTQ_DEV int32_t byte_of(const u32x4 *v, int i) { return (int32_t)(v[i >> 4][i >
 
 // PHASES 3: both, a tile a wavefront and its scores in registers; 1: keys only; 2: values only.
 // HALVES 2: up to eight queries share a kv head.  The second product's sixteen columns are then the upper halves of
-// eight queries' weights and the lower halves of the same: one product in place of two, and lanes that would have
-// been idle make the same weights as their neighbours.
+// eight queries' weights and the lower halves of the same: one product in place of two.  The two lanes of a query divide
+// the scores and weights of a block's 16 keys, eight each, and hand each other the halves of weights that they do not multiply with.
 // (One of 700 tokens 7.6 us, 64 of 4000 74, two of 65536 52; in the other form 7.8, 77 and 54.)
 // HALVES 1: sixteen queries, one product for either half.
 template <int D, int VARIANT, int HALVES, int PHASES>
@@ -89,6 +89,7 @@ struct CacheAttention {
     static constexpr int G = (D + kGroup - 1) / kGroup, PAIRS = D / 2, BLOCKS = D / 32;    // blocks of 16 channel pairs
     static constexpr int QUERIES = 16 / HALVES, PRODUCTS = 3 - HALVES;
     static constexpr int ACC = BLOCKS * 2 * 4 * 64;       // sums of 16 columns
+    static constexpr int OWN = 16 / HALVES;               // of a block's keys, the lane's
 
     // A tile's codes as the wavefront loads them, 16 bytes a lane in the order of the memory (a quarter of a
     // wavefront-wide load then meets whole lines; loaded in the products' order, every lane of a quad had a line of its own
@@ -194,22 +195,49 @@ struct CacheAttention {
         for (int b = 0; b < BLOCKS; ++b) *reinterpret_cast<u32x4 *>(stage + b * kValueBlock + at) = v.codes[b];
         wave_lds_fence();
     }
-    // Scores of a tile -> 16-bit differences from the tile's largest of the column (packed pairs), and that largest.
-    IPTQ_DEV void score(const Keys &k, int32_t at, uint32_t (&d)[8], int32_t *ref) const
+    IPTQ_DEV bool second() const { return HALVES == 2 && col >= 8; }      // the lane's keys are a block's last eight
+    // The steps of the lane's own keys, OWN * G bytes.
+    struct Steps { u32x4 v[OWN * G > 16 ? 2 : 1]; };
+    IPTQ_DEV Steps own_steps(const u32x4 (&steps)[G]) const
     {
-        int32_t x[16];
+        Steps t;
+        if (HALVES == 1) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) t.v[g] = steps[g];
+        } else if (G == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.v[0][i] = second() ? steps[G - 1][i] : steps[0][i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) t.v[0][i] = second() ? steps[0][2 + i] : steps[0][i];
+        }
+        return t;
+    }
+    static IPTQ_DEV int32_t other_half(int32_t v) { return __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, true); }      // row_ror:8
+    // Scores of a tile -> 16-bit differences from the tile's largest of the column (packed pairs), and that largest.
+    IPTQ_DEV void score(const Keys &k, int32_t at, uint32_t (&d)[OWN / 2], int32_t *ref) const
+    {
+        int32_t x[OWN];
         stage_keys(k);
+        const Steps steps = own_steps(k.steps);
         const int8_t *src = stage + keys_at(col >> 2) + (col & 3) * PAIRS + 8 * p;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < 4 / HALVES; ++s) {
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                // (where the last group is half a one, lanes 32 on take the others' codes, against zeros of the query)
-                const u32x2_t codes = *reinterpret_cast<const u32x2_t *>(src + (kGroup * g + 48 < D ? 0 : p >= 2 ? -16 : 0) + 4 * s * PAIRS + kGroup / 2 * g);
-                const i32x4 y = __builtin_amdgcn_mfma_i32_16x16x64_i8(upper_nibbles(codes), q[g], (i32x4){0, 0, 0, 0}, 0, 0, 0);
+                i32x4 y;
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) {
+                    // (where the last group is half a one, lanes 32 on take the others' codes, against zeros of the query)
+                    const u32x2_t codes = *reinterpret_cast<const u32x2_t *>(src + (kGroup * g + 48 < D ? 0 : p >= 2 ? -16 : 0) + 4 * (s + 2 * h) * PAIRS +
+                                                                             kGroup / 2 * g);
+                    const i32x4 z = __builtin_amdgcn_mfma_i32_16x16x64_i8(upper_nibbles(codes), q[g], (i32x4){0, 0, 0, 0}, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[r] = h == 0 || second() ? z[r] : y[r];
+                }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int32_t t = __mul24(byte_of(k.steps, (4 * s + r) * G + g), y[r]);
+                    const int32_t t = __mul24(byte_of(steps.v, (4 * s + r) * G + g), y[r]);
                     x[4 * s + r] = g ? x[4 * s + r] + t : t;
                 }
             }
@@ -217,69 +245,76 @@ struct CacheAttention {
         wave_lds_fence();                                 // the buffer may be written again
         // scores are 16 times their value: a shift of four more
         const int32_t shift = A.P.shift + 4, rounding = A.P.shift > 0 ? 1 << (shift - 1) : 0;
-        const int32_t seen = k.page >= 0 ? limit - (at + 16 * p) : 0;         // of the lane's 16 keys
-        const bool whole = __all(seen >= 16);
+        const int32_t seen = k.page >= 0 ? limit - (at + 16 * p + (second() ? 8 : 0)) : 0;       // of the lane's keys
+        const bool whole = __all(seen >= OWN);
         int32_t top = kI32Min;
         if (whole) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = max(top, x[i]);
+            for (int i = 0; i < OWN; ++i) top = max(top, x[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = i < seen ? max(top, x[i]) : top;
+            for (int i = 0; i < OWN; ++i) top = i < seen ? max(top, x[i]) : top;
         }
+        if (HALVES == 2) top = max(top, other_half(top));
         top = max(top, __shfl_xor(top, 16));
         top = max(top, __shfl_xor(top, 32));
         *ref = top == kI32Min ? kI32Min : (top + rounding) >> shift;
         const int32_t base = top == kI32Min ? 0 : rounding - (*ref << shift);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = (x[i] + base) >> shift;
+        for (int i = 0; i < OWN; ++i) x[i] = (x[i] + base) >> shift;
         if (!whole) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = i < seen ? x[i] : -32768;
+            for (int i = 0; i < OWN; ++i) x[i] = i < seen ? x[i] : -32768;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pk_i16(x[2 * i], x[2 * i + 1]));
+        for (int i = 0; i < OWN / 2; ++i) d[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pk_i16(x[2 * i], x[2 * i + 1]));
     }
     // One tile's share of the weighted values.
-    IPTQ_DEV void accumulate(const Values &v, const uint32_t (&d)[8], int32_t ref, int32_t top, i32x4 (&acc)[BLOCKS][2][PRODUCTS],
+    IPTQ_DEV void accumulate(const Values &v, const uint32_t (&d)[OWN / 2], int32_t ref, int32_t top, i32x4 (&acc)[BLOCKS][2][PRODUCTS],
                              uint32_t *sum) const
     {
         stage_values(v);
         const short off = (short)(ref == kI32Min ? -32768 : max(ref - top, -32768));
         const i16x2 least = {(short)-A.P.d_clamp, (short)-A.P.d_clamp}, offs = {off, off};
-        uint32_t w[8];
+        uint32_t w[OWN / 2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < OWN / 2; ++i) {
             const i16x2 t = __builtin_elementwise_max(__builtin_elementwise_add_sat(__builtin_bit_cast(i16x2, d[i]), offs), least);
             w[i] = __builtin_bit_cast(uint32_t, t);
         }
-        uint32_t (&w0)[4] = *reinterpret_cast<uint32_t (*)[4]>(w), (&w1)[4] = *reinterpret_cast<uint32_t (*)[4]>(w + 4);
-        weights_of_pairs<VARIANT, 4>(w0, A.P);
-        weights_of_pairs<VARIANT, 4>(w1, A.P);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) *sum = __builtin_amdgcn_udot2(__builtin_bit_cast(u16x2_t, w[i]), (u16x2_t){1, 1}, *sum, false);
+        for (int i = 0; i < OWN / 8; ++i) weights_of_pairs<VARIANT, 4>(*reinterpret_cast<uint32_t (*)[4]>(w + 4 * i), A.P);
+#pragma unroll
+        for (int i = 0; i < OWN / 2; ++i) *sum = __builtin_amdgcn_udot2(__builtin_bit_cast(u16x2_t, w[i]), (u16x2_t){1, 1}, *sum, false);
         // u = (w a + 64) >> 7 is the upper part of t = 2 w a + 128, from bit 8 on; with 128 more of u in it, its upper byte
         // is the upper half of u and its lower byte the lower half with the sign turned
-        i32x4 hi[G], lo[G];
-        const uint32_t select = HALVES == 2 && col >= 8 ? 0x06040200u : 0x07050301u, turn = HALVES == 2 && col < 8 ? 0u : 0x80808080u;
+        const Steps steps = own_steps(v.steps);
+        i32x4 hi[G], lo[G];                               // HALVES 2: hi is the half that the lane multiplies with
+        const uint32_t select = second() ? 0x06040200u : 0x07050301u, turn = second() ? 0x80808080u : 0u;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < OWN / 4; ++i) {
                 uint32_t u[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const u16x2_t w2 = __builtin_bit_cast(u16x2_t, w[2 * i + j]) << (unsigned short)1;
                     const int at0 = (4 * i + 2 * j) * G + g, at1 = at0 + G;           // the steps' bytes
-                    const uint32_t a = __builtin_amdgcn_perm(0u, v.steps[at0 >> 4][at0 >> 2 & 3], 0x0c0c0c00u | (at0 & 3));
-                    const uint32_t b = __builtin_amdgcn_perm(0u, v.steps[at1 >> 4][at1 >> 2 & 3], 0x0c000c0cu | (at1 & 3) << 16);
+                    const uint32_t a = __builtin_amdgcn_perm(0u, steps.v[at0 >> 4][at0 >> 2 & 3], 0x0c0c0c00u | (at0 & 3));
+                    const uint32_t b = __builtin_amdgcn_perm(0u, steps.v[at1 >> 4][at1 >> 2 & 3], 0x0c000c0cu | (at1 & 3) << 16);
                     const uint32_t ta = __builtin_amdgcn_udot2(w2, __builtin_bit_cast(u16x2_t, a), 128u + 32768u, false);
                     const uint32_t tb = __builtin_amdgcn_udot2(w2, __builtin_bit_cast(u16x2_t, b), 128u + 32768u, false);
                     u[j] = __builtin_amdgcn_perm(tb, ta, 0x06050201u);
                 }
-                hi[g][i] = (int32_t)__builtin_amdgcn_perm(u[1], u[0], select);
-                if (HALVES == 2) hi[g][i] = (int32_t)((uint32_t)hi[g][i] ^ turn);
-                else lo[g][i] = (int32_t)(__builtin_amdgcn_perm(u[1], u[0], 0x06040200u) ^ turn);
+                if (HALVES == 1) {
+                    hi[g][i] = (int32_t)__builtin_amdgcn_perm(u[1], u[0], 0x07050301u);
+                    lo[g][i] = (int32_t)(__builtin_amdgcn_perm(u[1], u[0], 0x06040200u) ^ 0x80808080u);
+                } else {
+                    const int32_t mine = (int32_t)(__builtin_amdgcn_perm(u[1], u[0], select) ^ turn);
+                    const int32_t given = other_half((int32_t)__builtin_amdgcn_perm(u[1], u[0], select ^ 0x01010101u)) ^ (int32_t)turn;
+                    hi[g][i & 1] = second() ? given : mine;
+                    hi[g][2 + (i & 1)] = second() ? mine : given;
+                }
             }
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
@@ -328,11 +363,11 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
     const int columns = A.columns, column = e_wg + (col & (T::QUERIES - 1));
     int16_t *deltas = A.deltas + pair * tiles * 4 * columns * 16;
     int32_t *refs = A.refs + pair * tiles * columns;
-    const bool mine = col < T::QUERIES && column < columns;                // the lane writes its column's scores
+    const bool mine = column < columns;                                    // the lane writes its column's scores
 
     // (PHASES 3) the values are on their way while the keys are worked on
     typename T::Values only;
-    uint32_t only_d[8];
+    uint32_t only_d[T::OWN / 2];
     int32_t only_ref = kI32Min;
     int32_t top = kI32Min;
     if (threadIdx.x < 16) lds_top[threadIdx.x] = kI32Min;
@@ -349,15 +384,15 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
             typename T::Keys now = t.load_keys(t.from);
             for (int32_t at = t.from; at < t.to; at += kTile) {
                 const typename T::Keys next = t.load_keys(min(at + kTile, (t.to - 1) & ~(kTile - 1)));
-                uint32_t d[8];
+                uint32_t d[T::OWN / 2];
                 int32_t ref;
                 t.score(now, at, d, &ref);
                 top = max(top, ref);
                 const int32_t tile = at / kTile;
                 if (mine) {
                     u32x4 *o = reinterpret_cast<u32x4 *>(deltas) + (int64_t)(tile * 4 + p) * 2 * columns + column;
-                    o[0] = (u32x4){d[0], d[1], d[2], d[3]};
-                    o[columns] = (u32x4){d[4], d[5], d[6], d[7]};
+                    o[t.second() ? columns : 0] = (u32x4){d[0], d[1], d[2], d[3]};
+                    if (HALVES == 1) o[columns] = (u32x4){d[T::OWN / 2 - 4], d[T::OWN / 2 - 3], d[T::OWN / 2 - 2], d[T::OWN / 2 - 1]};
                     if (p == 0) refs[tile * columns + column] = ref;
                 }
                 now = next;
@@ -396,10 +431,14 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
             t.accumulate(only, only_d, only_ref, top, acc, &sum);
         } else {
             const int from_column = min(column, columns - 1);
-            struct Scores { u32x4 a, b; int32_t ref; };
+            struct Scores { u32x4 v[2 / HALVES]; int32_t ref; };
             auto load_scores = [&](int32_t at) {
                 const u32x4 *o = reinterpret_cast<const u32x4 *>(deltas) + (int64_t)(at / kTile * 4 + p) * 2 * columns + from_column;
-                return (Scores){o[0], o[columns], refs[at / kTile * columns + from_column]};
+                Scores x;
+                x.v[0] = o[t.second() ? columns : 0];
+                if (HALVES == 1) x.v[2 / HALVES - 1] = o[columns];
+                x.ref = refs[at / kTile * columns + from_column];
+                return x;
             };
             typename T::Values now = t.load_values(t.from);
             Scores scores = load_scores(t.from);
@@ -407,13 +446,16 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
                 const int32_t ahead = min(at + kTile, (t.to - 1) & ~(kTile - 1));
                 const typename T::Values next = t.load_values(ahead);
                 const Scores further = load_scores(ahead);
-                const uint32_t d[8] = {scores.a.x, scores.a.y, scores.a.z, scores.a.w, scores.b.x, scores.b.y, scores.b.z, scores.b.w};
+                uint32_t d[T::OWN / 2];
+#pragma unroll
+                for (int i = 0; i < T::OWN / 2; ++i) d[i] = scores.v[i >> 2][i & 3];
                 t.accumulate(now, d, scores.ref, top, acc, &sum);
                 now = next;
                 scores = further;
             }
         }
         // the wavefronts' sums: whole numbers, so the order in which they are added does not matter
+        if (HALVES == 2) sum += (uint32_t)T::other_half((int32_t)sum);
         sum += (uint32_t)__shfl_xor((int32_t)sum, 16);
         sum += (uint32_t)__shfl_xor((int32_t)sum, 32);
         if (p == 0) atomicAdd(lds_sum + col, sum);
