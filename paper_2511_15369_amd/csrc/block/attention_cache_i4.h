@@ -298,12 +298,12 @@ struct CacheAttention {
                 uint32_t u[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const u16x2_t w2 = __builtin_bit_cast(u16x2_t, w[2 * i + j]) << (unsigned short)1;
-                    const int at0 = (4 * i + 2 * j) * G + g, at1 = at0 + G;           // the steps' bytes
-                    const uint32_t a = __builtin_amdgcn_perm(0u, steps.v[at0 >> 4][at0 >> 2 & 3], 0x0c0c0c00u | (at0 & 3));
-                    const uint32_t b = __builtin_amdgcn_perm(0u, steps.v[at1 >> 4][at1 >> 2 & 3], 0x0c000c0cu | (at1 & 3) << 16);
-                    const uint32_t ta = __builtin_amdgcn_udot2(w2, __builtin_bit_cast(u16x2_t, a), 128u + 32768u, false);
-                    const uint32_t tb = __builtin_amdgcn_udot2(w2, __builtin_bit_cast(u16x2_t, b), 128u + 32768u, false);
+                    const uint32_t w2 = __builtin_bit_cast(uint32_t, __builtin_bit_cast(u16x2_t, w[2 * i + j]) << (unsigned short)1);
+                    const int at0 = (4 * i + 2 * j) * G + g;
+                    uint32_t ta = __umul24(w2 & 0xffffu, (uint32_t)byte_of(steps.v, at0)), tb = __umul24(w2 >> 16, (uint32_t)byte_of(steps.v, at0 + G));
+                    asm("" : "+v"(ta), "+v"(tb));         // (kept from the addition, the products take their operands' halves and bytes as they lie)
+                    ta += 128u + 32768u;
+                    tb += 128u + 32768u;
                     u[j] = __builtin_amdgcn_perm(tb, ta, 0x06050201u);
                 }
                 if (HALVES == 1) {
