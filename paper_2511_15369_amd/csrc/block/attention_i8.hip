@@ -19,13 +19,19 @@ hipError_t attention_i8_dispatch(const AttentionCall &c, hipStream_t stream)
     a.by_seq = div_of((uint32_t)c.n_seq);
     a.P = c.P;
     a.post = narrow_post_of(c.P.post.m, c.P.post.s);
-    // Workgroups of 128 queries, or of 32 with their keys divided over the wavefronts where the former do not reach every
-    // compute unit: 197 tokens of 3 heads 6.0 us (128 queries: 9.5), 512 of 32 heads 20.1 (21.1), 4000 of 4 heads 55 (116), 8000 of 4
-    // heads, 252 workgroups, 178 (229); from 256 on the other way, 900 of 32 heads 44 (32), 2000 129 (65), 64 images of 49 9.1 (6.0).
+    // Workgroups of 128 queries, or of 32 with their keys divided over eight wavefronts.  In time of a block of 32 keys on a wavefront, with K blocks
+    // to a row and R workgroups of 32 queries to a compute unit: the latter take R (K / 4 + F), the former K + F while they find a compute
+    // unit each, F = 7.5 for the rest of a workgroup's life.  Causal rows are half as long on average, which only many short workgroups
+    // make use of: R (K / 8 + F).  So 32 queries where R is at most 1, or K (4 - R) > 4 F (R - 1), 8 in place of 4 for causal rows.
+    // Measured, us, 32 queries and 128: 197 tokens of 3 heads of 64 5.5 and 9.6, 512 of 32 heads of 128 16.9 and 21.3, 640 24.0 and 24.6, 900 38 and
+    // 33, 1500 74 and 51; 4000 of 8 heads 97 and 119, 8000 of 4 166 and 230, 16000 of 4 597 and 471; 8 sequences of 197, 12 heads of 64, 12.2 and
+    // 9.7, 32 of 49, 8 heads of 32, 5.1 and 4.8, 8 of 100, 32 heads of 128, 21 and 10.
     const uint32_t pairs = (uint32_t)c.n_seq * (uint32_t)c.heads;
-    a.tiles = ((uint32_t)c.max_q + kQueries - 1) / kQueries;
-    const bool few = (int64_t)a.tiles * pairs < 256;
-    if (few) a.tiles = ((uint32_t)c.max_q + 31) / 32;
+    const int64_t keys = std::max<int64_t>(c.max_q, c.k_tokens / c.n_seq), blocks = (keys + 31) / 32, spread = c.P.causal ? 8 : 4;
+    const int64_t of_32 = ((int64_t)c.max_q + 31) / 32 * pairs;
+    const bool few = of_32 <= 256 || 2 * blocks * (256 * spread - of_32) > 15 * spread * (of_32 - 256);
+    const uint32_t queries = few ? 32 : kQueries;
+    a.tiles = ((uint32_t)c.max_q + queries - 1) / queries;
     const uint32_t wgs = a.tiles * pairs;                 // below 2^31: checked
     for (a.first_wg = 0; a.first_wg < wgs; a.first_wg += kLaunchMost) {
         const uint32_t grid = std::min(wgs - a.first_wg, kLaunchMost);

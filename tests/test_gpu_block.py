@@ -71,7 +71,7 @@ def _packed(rng, q_lens, k_lens, heads, kv_heads, dim, p, fused=True, max_q=None
 @pytest.mark.parametrize("dim", [32, 64, 96, 128])
 @pytest.mark.parametrize("variant", [0, 1, 2])
 @pytest.mark.parametrize("causal", [0, 1])
-@pytest.mark.parametrize("heads", [6, 27])                # 10 sequences of up to two tiles: 120 tiles of 128 queries, and 540
+@pytest.mark.parametrize("heads", [3, 6, 27])             # 10 sequences of up to two tiles of 128 queries: either kernel
 def test_packed_lengths(dim, variant, causal, heads):
     """Lengths around the tiles' edges, sequences without queries, without keys, with fewer keys than queries."""
     rng = np.random.default_rng([dim, variant, causal, heads])
@@ -90,7 +90,7 @@ def test_heads(heads, kv_heads, dim):
 
 
 @pytest.mark.parametrize("n,dim,variant,heads", [(1000, 128, 0, 2), (1537, 64, 1, 2), (2111, 32, 2, 2), (700, 96, 1, 2), (1000, 128, 1, 32), (1537, 64, 0, 20),
-                                                 (1999, 32, 1, 16), (700, 96, 2, 48), (641, 128, 2, 48)])
+                                                 (1999, 32, 1, 16), (700, 96, 2, 48), (641, 128, 2, 48), (1537, 64, 1, 40), (1999, 32, 0, 40)])
 @pytest.mark.parametrize("causal", [0, 1])
 def test_long_prompts(n, dim, variant, heads, causal):
     rng = np.random.default_rng([n, causal])
