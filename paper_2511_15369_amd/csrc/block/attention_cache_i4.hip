@@ -79,13 +79,13 @@ static CachePlan plan_of(const CacheAttentionCall &c)
     const int64_t keys = (int64_t)c.max_pages * c.C.page_tokens;           // at most
     p.tiles = (int)((keys + kTile - 1) / kTile);
     // Up to 1024 keys: a tile a wavefront, up to sixteen of these, and all of a sequence's scores in registers: one launch (64 sequences of
-    // 1000 tokens, 32 heads on 8, 22.7 us, in two phases 34.8; one of 500 6.5 and 11.9).
+    // 1000 tokens, 32 heads on 8, 21.8 us, in two phases 34.8; one of 500 6.0 and 11.9).
     p.whole = keys <= 1024 && p.pairs * p.chunks <= (int64_t)kLaunchMost;
     p.key_waves = p.whole ? std::max(p.tiles, 1) : 4;
     p.splits = 1;
     if (!p.whole) {
         // A wavefront has 64 to 1024 keys.  Up to eight queries: twice as many workgroups as the chip holds, for the sake of sequences of
-        // different lengths (64 of 200 to 8192 tokens 75 us, with half as many workgroups 80; of equal lengths 4 % the other way: 64 of 4000 72
+        // different lengths (64 of 200 to 8192 tokens 75 us, with half as many workgroups 80; of equal lengths the other way: 64 of 4000 72 to 76
         // and 69).  More queries: once, as each split writes and reads a sum per column and channel (two of 65536 tokens, 32 columns, 76 and 93).
         const int64_t most = (keys + kTile * p.key_waves - 1) / (kTile * p.key_waves), least = (keys + 1024 * p.key_waves - 1) / (1024 * p.key_waves);
         const int64_t wanted = (columns > 8 ? 1024 : 2048) / (p.pairs * p.chunks);
@@ -150,7 +150,7 @@ hipError_t attention_cache_i4_dispatch(const CacheAttentionCall &c, hipStream_t 
     if (e != hipSuccess) return e;
     e = launch(a, p.halves, 2, grid, block, p.lds, stream);
     if (e != hipSuccess) return e;
-    // (4 splits, 64 sequences of 4000 tokens, 69 us, in the other form 74; 16 splits, 16 of 3000, 19.1 and 17.5; 128, one of 131072, 52 and 48)
+    // (4 splits, 64 sequences of 4000 tokens, 69 to 72 us, in the other form 74 to 76; 16 splits, 16 of 3000, 19.1 and 17.5; 128, one of 131072, 52 and 48)
     if (p.splits <= 8) launch_kernel(attention_cache_i4_join_kernel<4>, dim3((a.all_columns + 3) / 4), dim3(256), 0, stream, a);
     else launch_kernel(attention_cache_i4_join_kernel<16>, dim3(a.all_columns), dim3(256), 0, stream, a);
     return take_launch_status();

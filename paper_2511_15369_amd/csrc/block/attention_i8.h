@@ -334,8 +334,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const Atte
 }
 
 // Few queries: a workgroup has 32, and its wavefronts divide the keys, blocks of 32 in turn.  Each keeps to itself until
-// the maxima are joined, and again until the sums are: whole numbers, so their order does not matter.  Bound by latency: 197 tokens, 3
-// heads of 64, 21 workgroups of one block per wavefront, take 6.1 us, and a launch that does nothing about 2.3.
+// the maxima are joined, and again until the sums are: whole numbers, so their order does not matter.  (The sums change hands as rows of
+// LDS: 32 atomics a lane in their place took 0.5 us of 197 tokens' 6.)  Bound by latency: 197 tokens, 3 heads of 64, 21
+// workgroups of one block per wavefront, take 5.7 us; of their 10,000 cycles 2200 are the first loads, 1100 the scores, 2600 the weights and
+// their product, 2500 the two joins.
 constexpr int kFewWaves = 8;
 
 // The wavefronts' tiles, and in the same place their sums of weighted values at the end; the maxima, the sums of the weights.

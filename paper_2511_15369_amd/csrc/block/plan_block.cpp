@@ -69,7 +69,7 @@ extern "C" int iptq_attention_i8(const int8_t *d_q, int64_t q_stride, const int8
     if (rc != IPTQ_OK) return rc;
     rc = check_heads(heads, kv_heads, head_dim);
     if (rc != IPTQ_OK) return rc;
-    const int64_t tokens_most = (int64_t)1 << 31;
+    const int64_t tokens_most = ((int64_t)1 << 31) - 256;        // (rows are counted past a tile's last in 32 bits)
     if (n_seq < 0 || max_q < 0 || q_tokens < 0 || k_tokens < 0 || q_tokens >= tokens_most || k_tokens >= tokens_most)
         return IPTQ_ERR_SHAPE;
     const int64_t qw = (int64_t)heads * head_dim, kw = (int64_t)kv_heads * head_dim, stride_most = (int64_t)1 << 31;

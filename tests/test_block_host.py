@@ -39,7 +39,7 @@ def attention(p=params(), stream=None, **k):
     (PARAM, dict(p=params(score_shift=-1))), (PARAM, dict(p=params(causal=2))), (PARAM, dict(p=params(variant=3))),
     (PARAM, dict(p=params(post=ip.Dyadic(1, 63, 0, -128, 127)))), (PARAM, dict(p=params(post=ip.Dyadic(1, 0, 0, 0, 255)))),
     (SHAPE, dict(heads=0)), (SHAPE, dict(heads=7)), (SHAPE, dict(kv=0)), (SHAPE, dict(dim=48)), (SHAPE, dict(dim=256)), (SHAPE, dict(n=-1)),
-    (SHAPE, dict(max_q=-1)), (SHAPE, dict(qt=-1)), (SHAPE, dict(kt=1 << 31)), (SHAPE, dict(qs=511)), (SHAPE, dict(ks=127)),
+    (SHAPE, dict(max_q=-1)), (SHAPE, dict(qt=-1)), (SHAPE, dict(kt=1 << 31)), (SHAPE, dict(qt=(1 << 31) - 256)), (NULL, dict(n=1, qt=(1 << 31) - 257, q=None)), (SHAPE, dict(qs=511)), (SHAPE, dict(ks=127)),
     (SHAPE, dict(vs=127)), (SHAPE, dict(os=511)), (SHAPE, dict(os=1 << 31)), (NULL, dict(qo=None)), (NULL, dict(ko=None)),
     (SHAPE, dict(qo=None, ko=None)), (SHAPE, dict(qo=None, ko=None, n=3)), (SHAPE, dict(qo=None, ko=None, n=1, kt=65537)),
     (0, dict(qo=None, ko=None, n=0, qt=0, kt=0)), (0, dict(n=1, max_q=0)), (0, dict(n=1, qt=0)), (SHAPE, dict(n=1 << 30, max_q=1 << 20)),
