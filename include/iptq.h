@@ -354,8 +354,8 @@ typedef struct {
 /*
  * Attention over packed sequences.  d_q: q_tokens rows of heads * head_dim int8, q_stride bytes apart; d_k, d_v:
  * k_tokens rows of kv_heads * head_dim, k_stride and v_stride apart (so all three may lie in the rows of one
- * product's output; both counts below 2^31 - 256); d_out as d_q with out_stride.  No alignment is asked.  heads is a multiple of kv_heads, head h
- * reads the keys of head h div (heads / kv_heads).  head_dim: 32, 64, 96 or 128.
+ * product's output); d_out as d_q with out_stride.  Both counts are below 2^31 - 256.  No alignment is asked.  heads is a
+ * multiple of kv_heads, head h reads the keys of head h div (heads / kv_heads).  head_dim: 32, 64, 96 or 128.
  * Sequence i has queries d_q_offsets[i] .. d_q_offsets[i + 1] - 1 and keys d_k_offsets[i] .. d_k_offsets[i + 1] - 1
  * (n_seq + 1 int32 each, device, not decreasing); both NULL: equal lengths, q_tokens / n_seq and k_tokens / n_seq (no
  * remainder, else IPTQ_ERR_SHAPE).  causal: the last query of a sequence sees all its keys, the one before it all but the last,

@@ -485,7 +485,7 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
         const int channel = 32 * b + 8 * (l >> 4);
         if (PHASES == 3) {
             const uint32_t token = div_by(x, A.by_group), head = kvh * (uint32_t)A.group + (x - token * (uint32_t)A.group);
-            store_means(A.out + t.q_row(token) * A.out_stride + head * D + channel, floor_div_u64((uint64_t)1 << 54, s), v, A.P);
+            store_means(A.out + t.q_row(token) * A.out_stride + head * D + channel, floor_div_scaled(1, 54, s), v, A.P);
         } else {
             const int64_t at = (pair * A.splits + split) * A.columns + x;
             i32x4 *o = reinterpret_cast<i32x4 *>(A.partial + at * D + channel);

@@ -53,7 +53,7 @@ __global__ __launch_bounds__(256) void attention_cache_i4_join_kernel(const Cach
         s = totals[0] + totals[1] + totals[2] + totals[3];
     }
     if (part != 0 || 8 * unit >= dim) return;
-    const uint64_t f = floor_div_u64((uint64_t)1 << 54, s);
+    const uint64_t f = floor_div_scaled(1, 54, s);
     const uint32_t token = div_by(column, A.by_group), head = kvh * (uint32_t)A.group + (column - token * (uint32_t)A.group);
     store_means(A.out + ((int64_t)seq * A.q_tokens + token) * A.out_stride + head * dim + 8 * unit, f, v, A.P);
 }

@@ -322,7 +322,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const Atte
     }
     sum += (uint32_t)__shfl_xor((int32_t)sum, 32);
     if (row >= nq) return;
-    const uint64_t f = floor_div_u64((uint64_t)1 << 54, sum);
+    const uint64_t f = floor_div_scaled(1, 54, sum);
     int8_t *out = A.out + (int64_t)(T.q0 + row) * A.out_stride + T.head * D;
     if (__all(sum < 1u << 24)) {
 #pragma unroll
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void attention_i8_few_kernel(const 
         uint32_t sum = 0;
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) sum += w < waves ? lds_sum[32 * w + q] : 0;
-        return floor_div_u64((uint64_t)1 << 54, sum);
+        return floor_div_scaled(1, 54, sum);
     };
     auto store = [&](int m, int32_t bytes) {
         const int u = threadIdx.x + 64 * kFewWaves * m, i = u >> 6 & 3, s = u >> 8;

@@ -120,26 +120,41 @@ hipError_t rmsnorm_i32_dispatch(const RmsnormCall &c, hipStream_t stream);
 hipError_t requant_rows_dispatch(const int32_t *in, const int32_t *row_scales, int32_t row_shift, void *out, int64_t rows,
                                  int32_t cols, const DyadicDev &P, hipStream_t stream);
 
-// floor(num / den), num < 2^63, den >= 1 (0 for den == 0): quotients by a 32-bit reciprocal of den that is
-// never too large (Newton's iteration, as floor_pow2_div), the remainder divided again until it is below
-// den.  A step leaves less than 2^-27 of the remainder, so three or four do.
-IPTQ_HD uint64_t floor_div_u64(uint64_t num, uint32_t den)
+// 2^63 / (den << k), k the zeros in front of den >= 1: never above it and at most 6 below (Newton's iteration, as floor_pow2_div;
+// within 2 of it for every y, less 4).
+IPTQ_HD uint32_t reciprocal_of(uint32_t den, int k)
 {
-    if (den == 0) return 0;
-    const int k = clz_u32(den);
     const uint32_t y = den << k;
     uint32_t r = (3031741620u - mulhi_u32(y, 2021161080u)) << 1;
     for (int it = 0; it < 3; ++it) r = mulhi_u32(r, 0u - mulhi_u32(y, r)) << 1;
-    r -= 4;                                               // within 2 of 2^63 / y for every y: never above it from here on
-    uint64_t q = 0;
-    while (num >= den) {
-        const uint64_t p = (num >> 32) * r + (((num & 0xffffffffu) * r) >> 32);     // num r / 2^32
-        uint64_t e = p >> (31 - k);
-        e = e == 0 ? 1 : e;
-        q += e;
-        num -= e * den;
+    return r - 4;
+}
+
+// floor(2^61 / den) for 2^30 <= den < 2^31: half of the reciprocal is at most four short.
+IPTQ_HD uint32_t floor_div_2_61(uint32_t den)
+{
+    uint32_t q = reciprocal_of(den, 1) >> 1;
+    uint64_t left = ((uint64_t)1 << 61) - (uint64_t)q * den;
+    while (left >= den) {
+        left -= den;
+        ++q;
     }
     return q;
+}
+
+// floor(c 2^n / den) for 32 <= n, c 2^n <= 2^54, den < 2^31 (0 for den == 0): the reciprocal is the first quotient, shifted; what it leaves
+// is below den + 6 c 2^(n - 31) < 2^32, so its low word, that of -q den, is all of it, and one more quotient is at most one short.
+IPTQ_HD uint64_t floor_div_scaled(uint32_t c, int n, uint32_t den)
+{
+    if (den == 0) return 0;
+    const int k = clz_u32(den), down = 63 - n - k;
+    const uint32_t r = reciprocal_of(den, k);
+    uint64_t q = (uint64_t)r * c;
+    q = down >= 0 ? q >> down : q << -down;
+    uint32_t left = 0u - (uint32_t)q * den;
+    const uint32_t e = mulhi_u32(left, r) >> (31 - k);
+    left -= e * den;
+    return q + e + (left >= den ? 1 : 0);
 }
 
 // floor(sqrt(v)) for 2^60 <= v < 2^62: Newton's iteration for 1 / sqrt(a), a = v / 2^62 in [1/4, 1), in 32 bits, one step of the

@@ -37,7 +37,7 @@ IPTQ_DEV uint32_t row_factor(uint64_t total, uint32_t root_cols, int *t)
     const uint32_t top = (uint32_t)(total >> 32);
     const int bits = top != 0 ? 64 - clz_u32(top) : 32 - clz_u32((uint32_t)total);
     *t = (62 - bits) >> 1;
-    const uint32_t inverse = (uint32_t)floor_div_u64((uint64_t)1 << 61, root_u62(total << (2 * *t)));
+    const uint32_t inverse = floor_div_2_61(root_u62(total << (2 * *t)));
     return (uint32_t)(((uint64_t)root_cols * inverse) >> 24);
 }
 IPTQ_DEV uint64_t at_most_62_bits(uint64_t v) { return v >= ((uint64_t)1 << 62) ? ((uint64_t)1 << 62) - 1 : v; }
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rmsnorm_i32_ker
         }
         if (tid == 0) A.row_scales[row] = (int32_t)most;
         // y f / 2^40 with f = floor(127 2^40 / most): y's and f's upper parts carry it, but the rounding wants all of it
-        const uint64_t f = floor_div_u64((uint64_t)127 << 40, most);
+        const uint64_t f = floor_div_scaled(127, 40, most);
 #pragma unroll
         for (int i = 0; i < CHUNKS; ++i) {
             int32_t code[4];
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256) void rmsnorm_narrow_kernel(const RmsnormArgs A
         most = max(most, (uint32_t)max(r[i], -r[i]));
     }
     if (A.row_scales) A.row_scales[row] = (int32_t)most;
-    const uint64_t f = A.row_scales ? floor_div_u64((uint64_t)127 << 40, most) : 0;
+    const uint64_t f = A.row_scales ? floor_div_scaled(127, 40, most) : 0;
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
         if (i >= A.cols) break;

@@ -266,16 +266,14 @@ static uint64_t s = 0x9E3779B97F4A7C15ull;
 static uint64_t rnd() { s ^= s << 13; s ^= s >> 7; s ^= s << 17; return s; }
 int main()
 {
-    for (long i = 0; i < 3000000; ++i) {
-        uint64_t n = rnd() >> (1 + rnd() % 63);
-        const uint32_t d = (uint32_t)(rnd() >> (32 + rnd() % 32));
-        if (i % 3 == 0) n = 1ull << 54;
-        if (i % 7 == 0) n = 127ull << 40;
-        if (i % 11 == 0) n = 1ull << 61;
-        if (floor_div_u64(n, d) != (d ? n / d : 0)) return printf("%llu / %u\n", (unsigned long long)n, d), 1;
+    for (long i = 0; i < 4000000; ++i) {
+        const uint32_t d = (1u << 30) | (uint32_t)(i < 100000 ? i : i < 200000 ? 0x3fffffffl - (i - 100000) : (long)(rnd() >> 34));
+        if (floor_div_2_61(d) != (1ull << 61) / d) return printf("%u\n", d), 1;
     }
-    for (uint32_t d = 1; d < 300000; ++d)
-        if (floor_div_u64(1ull << 54, d) != (1ull << 54) / d || floor_div_u64(1ull << 54, 0u - d) != (1ull << 54) / (0u - d)) return 2;
+    for (long i = 0; i < 4000000; ++i) {
+        const uint32_t d = i < 600000 ? (uint32_t)i : i < 700000 ? 0x7fffffffu - (uint32_t)(i - 600000) : (uint32_t)(rnd() >> (33 + rnd() % 31));
+        if (floor_div_scaled(1, 54, d) != (d ? (1ull << 54) / d : 0) || floor_div_scaled(127, 40, d) != (d ? (127ull << 40) / d : 0)) return printf("%u\n", d), 9;
+    }
     for (long i = 0; i < 300000; ++i) {
         const uint64_t v = i < 4 ? (1ull << 62) - 1 - i : i < 8 ? (1ull << 60) + i - 4 : (1ull << 60) + rnd() % (3ull << 60);
         const unsigned __int128 r = root_u62(v);
