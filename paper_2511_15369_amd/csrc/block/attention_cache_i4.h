@@ -371,6 +371,7 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
     uint32_t only_d[T::OWN / 2];
     int32_t only_ref = kI32Min;
     int32_t top = kI32Min;
+    const int32_t last = (t.to - 1) & ~(kTile - 1);                        // the wavefront's last tile
     if (threadIdx.x < 16) lds_top[threadIdx.x] = kI32Min;
     if (PHASES & 2)
         for (int i = threadIdx.x; i < 16 + T::ACC; i += blockDim.x) lds_top[16 + i] = 0;       // sums
@@ -382,21 +383,26 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
             top = only_ref;
         }
         if (PHASES == 1 && t.from < t.to) {
-            typename T::Keys now = t.load_keys(t.from);
-            for (int32_t at = t.from; at < t.to; at += kTile) {
-                const typename T::Keys next = t.load_keys(min(at + kTile, (t.to - 1) & ~(kTile - 1)));
+            auto step = [&](const typename T::Keys &keys, int32_t at) {
                 uint32_t d[T::OWN / 2];
                 int32_t ref;
-                t.score(now, at, d, &ref);
+                t.score(keys, at, d, &ref);
                 top = max(top, ref);
                 const int32_t tile = at / kTile;
-                if (mine) {
-                    u32x4 *o = reinterpret_cast<u32x4 *>(deltas) + (int64_t)(tile * 4 + p) * 2 * columns + column;
-                    o[t.second() ? columns : 0] = (u32x4){d[0], d[1], d[2], d[3]};
-                    if (HALVES == 1) o[columns] = (u32x4){d[T::OWN / 2 - 4], d[T::OWN / 2 - 3], d[T::OWN / 2 - 2], d[T::OWN / 2 - 1]};
-                    if (p == 0) refs[tile * columns + column] = ref;
-                }
-                now = next;
+                if (!mine) return;
+                u32x4 *o = reinterpret_cast<u32x4 *>(deltas) + (int64_t)(tile * 4 + p) * 2 * columns + column;
+                o[t.second() ? columns : 0] = (u32x4){d[0], d[1], d[2], d[3]};
+                if (HALVES == 1) o[columns] = (u32x4){d[T::OWN / 2 - 4], d[T::OWN / 2 - 3], d[T::OWN / 2 - 2], d[T::OWN / 2 - 1]};
+                if (p == 0) refs[tile * columns + column] = ref;
+            };
+            // (two tiles a trip: no copies from the next one's registers)
+            typename T::Keys ka = t.load_keys(t.from), kb;
+            for (int32_t at = t.from; at < t.to; at += 2 * kTile) {
+                kb = t.load_keys(min(at + kTile, last));
+                step(ka, at);
+                if (at + kTile >= t.to) break;
+                ka = t.load_keys(min(at + 2 * kTile, last));
+                step(kb, at + kTile);
             }
         }
         __syncthreads();
@@ -441,18 +447,22 @@ IPTQ_DEV void cache_attention_body(const CacheAttentionArgs &A, uint32_t kvh, ui
                 x.ref = refs[at / kTile * columns + from_column];
                 return x;
             };
-            typename T::Values now = t.load_values(t.from);
-            Scores scores = load_scores(t.from);
-            for (int32_t at = t.from; at < t.to; at += kTile) {
-                const int32_t ahead = min(at + kTile, (t.to - 1) & ~(kTile - 1));
-                const typename T::Values next = t.load_values(ahead);
-                const Scores further = load_scores(ahead);
+            typename T::Values va = t.load_values(t.from), vb;
+            Scores sa = load_scores(t.from), sb;
+            auto step = [&](const typename T::Values &v, const Scores &x) {
                 uint32_t d[T::OWN / 2];
 #pragma unroll
-                for (int i = 0; i < T::OWN / 2; ++i) d[i] = scores.v[i >> 2][i & 3];
-                t.accumulate(now, d, scores.ref, top, acc, &sum);
-                now = next;
-                scores = further;
+                for (int i = 0; i < T::OWN / 2; ++i) d[i] = x.v[i >> 2][i & 3];
+                t.accumulate(v, d, x.ref, top, acc, &sum);
+            };
+            for (int32_t at = t.from; at < t.to; at += 2 * kTile) {
+                vb = t.load_values(min(at + kTile, last));
+                sb = load_scores(min(at + kTile, last));
+                step(va, sa);
+                if (at + kTile >= t.to) break;
+                va = t.load_values(min(at + 2 * kTile, last));
+                sa = load_scores(min(at + 2 * kTile, last));
+                step(vb, sb);
             }
         }
         // the wavefronts' sums: whole numbers, so the order in which they are added does not matter
