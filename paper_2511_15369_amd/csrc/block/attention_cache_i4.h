@@ -145,6 +145,16 @@ struct CacheAttention {
         Keys k;
         const CacheDev &C = A.C;
         const int first = (at - from) >> 4, mask = C.page_tokens - 1;
+        if (C.page_log >= 6) {                            // a tile lies in one page: one address (64 of 1000 tokens 20.3 us, block by block 21.8)
+            k.page = __builtin_amdgcn_readlane(page_of_block, first);
+            const int64_t row = ((int64_t)max(k.page, 0) * C.kv_heads + kvh) * C.page_tokens + (at & mask);
+            const uint8_t *codes = C.k_codes + row * PAIRS + 16 * lane, *steps = C.k_steps + (row + 16 * p) * G;
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) k.codes[i] = *reinterpret_cast<const u32x4 *>(codes + 1024 * i);
+#pragma unroll
+            for (int g = 0; g < G; ++g) k.steps[g] = *reinterpret_cast<const u32x4 *>(steps + 16 * g);
+            return k;
+        }
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {                // (a key's row is BLOCKS chunks of 16 bytes)
             const int chunk = 64 * i + lane, block = chunk / (16 * BLOCKS), in_block = chunk - block * 16 * BLOCKS;
@@ -178,6 +188,16 @@ struct CacheAttention {
         int l = lane;
         asm volatile("" : "+v"(l));                       // (made again each time: kept, it may spill)
         const int first = (at - from) >> 4, mask = C.page_tokens - 1, block = value_block(l);
+        if (C.page_log >= 6) {
+            const int64_t head = (int64_t)max(__builtin_amdgcn_readlane(page_of_block, first), 0) * C.kv_heads + kvh;
+            const uint8_t *codes = C.v_codes + head * PAIRS * C.page_tokens + (at & mask) + (value_pair(l) * C.page_tokens + 16 * block);
+            const uint8_t *steps = C.v_steps + (head * C.page_tokens + (at & mask) + 16 * p) * G;
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) v.codes[b] = *reinterpret_cast<const u32x4 *>(codes + 16 * b * C.page_tokens);
+#pragma unroll
+            for (int g = 0; g < G; ++g) v.steps[g] = *reinterpret_cast<const u32x4 *>(steps + 16 * g);
+            return v;
+        }
         const int64_t head_at = (int64_t)max(__shfl(page_of_block, first + block), 0) * C.kv_heads + kvh;
         const uint8_t *src = C.v_codes + (head_at * PAIRS + value_pair(l)) * C.page_tokens + ((at + 16 * block) & mask);
 #pragma unroll
