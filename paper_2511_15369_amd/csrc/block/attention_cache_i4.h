@@ -8,9 +8,9 @@
 // before the first of them, so there are two phases, keys and then values, with the scores kept
 // between them: as 16-bit differences from the largest score of their 64-key tile and column, saturated (a score
 // that far below the maximum has weight 0 either way).  Their 2 bytes per key and column, written and read, are as many as the cache's
-// from 32 columns on, and the values' phase has 350 vector instructions per 64 keys and 16 columns.
-// Measured: 64 sequences of 200 to 8192 tokens, 32 heads on 8 of 128, 66 us (2.8 TB/s of cache; 30 us keys, 31 values, 5 the sum of
-// the splits); two of 131072, 32 columns, 139 us (2.0 TB/s of cache, 3.9 with the scores; 54, 80, 6); one of 700, 7.1 us with the call.
+// from 32 columns on, and the values' phase has 310 vector instructions per 64 keys and 16 columns (210 per 8).
+// Measured: 64 sequences of 200 to 8192 tokens, 32 heads on 8 of 128, 63 us (3.0 TB/s of cache; 28 us keys, 31 values, 5 the sum of
+// the splits); two of 131072, 32 columns, 136 us (2.0 TB/s of cache, 4.0 with the scores; 55, 80, 6); one of 700, 7 us with the call.
 //
 // Columns are the queries that share a kv head: e = token * group + head of the group, 16 of them to the narrow
 // side of v_mfma_i32_16x16x64_i8.  Keys go by tiles of 64, in blocks of 16 that never cross a page.  Scores are
@@ -82,7 +82,7 @@ IPTQ_DEV int32_t byte_of(const u32x4 *v, int i) { return (int32_t)(v[i >> 4][i >
 // HALVES 2: up to eight queries share a kv head.  The second product's sixteen columns are then the upper halves of
 // eight queries' weights and the lower halves of the same: one product in place of two.  The two lanes of a query divide
 // the scores and weights of a block's 16 keys, eight each, and hand each other the halves of weights that they do not multiply with.
-// (One of 1000 tokens, 4 queries, 7.8 us, 64 of 4000 65, one of 131072 45; with all the keys in both lanes 8.9, 72 and 48, with a
+// (One of 1000 tokens, 4 queries, 7.9 us, 64 of 4000 67, one of 131072 45; with all the keys in both lanes 8.9, 72 and 48, with a
 // product for either half a few per cent more.)
 // HALVES 1: sixteen queries, one product for either half.
 template <int D, int VARIANT, int HALVES, int PHASES>

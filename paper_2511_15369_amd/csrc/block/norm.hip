@@ -1,7 +1,7 @@
 // Root-mean-square norm with the residual's addition, and requantization by row scales.
 //
 // Both are bound by HBM: 13 bytes per value of the norm (product, residual, its new value, code), 5 of the requantization.
-// 8192 rows of 5120 take 97 us (5.6 TB/s), 8192 of 6144 requantized 40.5 us (6.2 TB/s); 64 rows, 4.5 and 3.8 us, are the launch.
+// 8192 rows of 5120 take 97 us (5.6 TB/s), 8192 of 6144 requantized 40.5 us (6.2 TB/s); 64 rows of either, 4.4 and 3.8 us, are the call.
 // A row stays in the registers of the wavefronts that hold it, so every byte crosses once.  Rows are read in chunks of four
 // values at their natural alignment; where four does not divide a row its last chunk ends with it and starts
 // earlier, and the values it shares with the chunk before count once.

@@ -320,6 +320,16 @@ def test_cache_attention_longest():
     _attend(rng, [n, 3], 2, 1, 32, page, 1, p)
 
 
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+@pytest.mark.parametrize("page,heads", [(16, 5), (32, 3), (128, 4), (256, 20), (4096, 9)])
+def test_cache_attention_page_sizes(dim, page, heads):
+    """Tiles of several pages, of one, pages of many tiles; over one workgroup and several."""
+    rng = np.random.default_rng([dim, page])
+    p = _attention(rng, dim, _spread(dim), 1, 1, cache=True)
+    _attend(rng, [900, 641, 63, 130], heads, 1, dim, page, 1, p)
+    _attend(rng, [4500, 4097, 1, 2111], heads, 1, dim, page, 2, p, spare=1)
+
+
 def test_cache_attention_pages_that_are_not_there():
     """Tokens in a page outside the cache count as masked; a sequence of such pages sees nothing."""
     rng = np.random.default_rng(4)
