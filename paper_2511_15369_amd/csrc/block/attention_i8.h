@@ -11,8 +11,8 @@
 //
 // Bound by the issue of vector and matrix instructions: 16 products of 32 x 32 x 32 per 32 queries and 32 keys (4 for the maximum, 4
 // for the scores, 8 for the values' two halves) and about 180 vector instructions, of two wavefronts per SIMD, which is as many as
-// 256 registers allow.  One prompt of 8192 tokens, 32 heads on 8 of 128, causal: 625 to 645 us, 1.7 POP/s of products done, four fifths of
-// what a large library product of int8 reaches; matrix units 34 % busy, vector units 55 %.  24 prompts of 17 to 1900 tokens: 195 us.
+// 256 registers allow.  One prompt of 8192 tokens, 32 heads on 8 of 128, causal: 620 to 640 us, 1.7 POP/s of products done, four fifths of
+// what a large library product of int8 reaches; matrix units 34 % busy, vector units 55 %.  24 prompts of 17 to 1900 tokens: 190 us.
 // Weights from a table in LDS in place of the arithmetic (half or none of the vector work) gave 3.5 and 5 % at 22 KB more LDS per
 // workgroup; a third tile buffer, wavefront priorities, scores of all 128 queries by each wavefront for a quarter of the keys gave nothing.
 //
@@ -43,14 +43,15 @@ struct AttentionArgs {
     int64_t q_stride, k_stride, v_stride, out_stride;
     const int32_t *q_offsets, *k_offsets;
     int32_t q_tokens, k_tokens, q_len, k_len, max_q;      // q_len, k_len: of every sequence where there are no offsets
-    DivDev by_kv_heads, by_group, by_seq;                 // workgroup number -> kv head, head of its group, sequence, tile
+    DivDev by_kv_heads, by_group, by_seq;                 // workgroup number -> kv head, heads of its group, sequence, tile
+    int32_t together;                                     // log2 of the heads of a group that a workgroup takes
     uint32_t tiles;
     uint32_t first_wg;                                    // of this launch
     AttentionDev P;
     NarrowPost post;
 };
 
-constexpr int kWaves = 4;             // 32 queries each
+constexpr int kWaves = 4;             // 32 queries each, of one head or of several that share a kv head
 constexpr int kQueries = 32 * kWaves;
 constexpr int kKeys = 64;             // keys per staged tile
 
@@ -100,8 +101,10 @@ IPTQ_DEV bool attention_tile(const AttentionArgs &A, uint32_t wg, int queries, A
     const uint32_t r1 = div_by(wg, A.by_kv_heads);
     t->kvh = wg - r1 * A.by_kv_heads.d;
     const uint32_t r2 = div_by(r1, A.by_group);
-    t->head = t->kvh * A.by_group.d + (r1 - r2 * A.by_group.d);
-    const uint32_t r3 = div_by(r2, A.by_seq), seq = r2 - r3 * A.by_seq.d;
+    t->head = (t->kvh * A.by_group.d + (r1 - r2 * A.by_group.d)) << A.together;
+    // (sequences change places from tile to tile: workgroups go to the chip's parts in turn, and a long sequence in the same place every time
+    // would keep meeting the same ones: 24 of 17 to 1900 tokens, 32 queries of four heads a workgroup, 404 us, so 190.)
+    const uint32_t r3 = div_by(r2, A.by_seq), turned = r2 - r3 * A.by_seq.d + r3, seq = turned - div_by(turned, A.by_seq) * A.by_seq.d;
     t->first = (int32_t)(A.tiles - 1 - r3) * queries;     // the longest rows first
     if (A.q_offsets) {
         clamped_range(A.q_offsets[seq], A.q_offsets[seq + 1], A.q_tokens, &t->q0, &t->nq);
@@ -176,21 +179,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const Atte
     __shared__ __attribute__((aligned(16))) int8_t lds_v[2][kKeys * VROW];
 
     AttentionTile T;
-    if (!attention_tile(A, A.first_wg + blockIdx.x, kQueries, &T)) return;
+    const int queries = kQueries >> A.together;
+    if (!attention_tile(A, A.first_wg + blockIdx.x, queries, &T)) return;
     const int32_t nq = T.nq, nk = T.nk;
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int32_t first = T.first + 32 * wave;        // the wavefront's first query
+    const int32_t first = T.first + (32 * wave & (queries - 1));      // the wavefront's first query
+    const uint32_t head = T.head + (uint32_t)(wave >> (2 - A.together));
     const int32_t row = first + col;
     const int32_t limit = A.P.causal ? min(max(row + T.diag + 1, 0), nk) : nk;
     // keys that any / every row of the wavefront sees, and that any row of the workgroup sees
     const int32_t wave_most = first >= nq ? 0 : A.P.causal ? min(max(min(first + 32, nq) + T.diag, 0), nk) : nk;
     const int32_t wave_least = A.P.causal ? min(max(first + T.diag + 1, 0), nk) : nk;
-    const int32_t most = A.P.causal ? min(max(min(T.first + kQueries, nq) + T.diag, 0), nk) : nk;
+    const int32_t most = A.P.causal ? min(max(min(T.first + queries, nq) + T.diag, 0), nk) : nk;
 
     i32x4 qf[STEPS];
     {
-        const int8_t *p = A.q + (int64_t)(T.q0 + min(row, nq - 1)) * A.q_stride + T.head * D + 16 * half;
+        const int8_t *p = A.q + (int64_t)(T.q0 + min(row, nq - 1)) * A.q_stride + head * D + 16 * half;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const i32x4_a1 *>(p + 32 * s);
     }
@@ -323,7 +328,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_i8_kernel(const Atte
     sum += (uint32_t)__shfl_xor((int32_t)sum, 32);
     if (row >= nq) return;
     const uint64_t f = floor_div_scaled(1, 54, sum);
-    int8_t *out = A.out + (int64_t)(T.q0 + row) * A.out_stride + T.head * D;
+    int8_t *out = A.out + (int64_t)(T.q0 + row) * A.out_stride + head * D;
     if (__all(sum < 1u << 24)) {
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) store_block<true>(out + 32 * s, f, acc_hi[s], acc_lo[s], half, A);

@@ -15,7 +15,6 @@ hipError_t attention_i8_dispatch(const AttentionCall &c, hipStream_t stream)
     a.q_len = (int32_t)(c.q_tokens / c.n_seq); a.k_len = (int32_t)(c.k_tokens / c.n_seq);
     a.max_q = c.max_q;
     a.by_kv_heads = div_of((uint32_t)c.kv_heads);
-    a.by_group = div_of((uint32_t)(c.heads / c.kv_heads));
     a.by_seq = div_of((uint32_t)c.n_seq);
     a.P = c.P;
     a.post = narrow_post_of(c.P.post.m, c.P.post.s);
@@ -30,9 +29,18 @@ hipError_t attention_i8_dispatch(const AttentionCall &c, hipStream_t stream)
     const int64_t keys = std::max<int64_t>(c.max_q, c.k_tokens / c.n_seq), blocks = (keys + 31) / 32, spread = c.P.causal ? 8 : 4;
     const int64_t of_32 = ((int64_t)c.max_q + 31) / 32 * pairs;
     const bool few = of_32 <= 256 || 2 * blocks * (256 * spread - of_32) > 15 * spread * (of_32 - 256);
-    const uint32_t queries = few ? 32 : kQueries;
+    // The wavefronts of the others take 32 queries of four heads, or 64 of two, where a group of heads has them: all read the same keys, and
+    // rows of like length leave none waiting for another and fewer places empty behind a sequence's last row.  That counts
+    // where there are more workgroups than the chip holds at once, two to a compute unit, or no second 128 queries: us, four heads and one, 64
+    // sequences of 200, 32 heads on 8 of 128, 85 and 106, 4 of 700 36 and 41, one of 3000 110 and 117, 64 of 49, 8 heads of 32, 5.0 and 5.9; one of
+    // 2000, 512 workgroups, 66.4 and 66.1, of 900 36.3 and 33.5, 4 of 300 16.7 and 15.0, where fewer wavefronts do all the work at once.
+    const uint32_t group = (uint32_t)(c.heads / c.kv_heads);
+    const bool shared = !few && (c.max_q <= kQueries || ((int64_t)c.max_q + kQueries - 1) / kQueries * pairs > 512);
+    a.together = !shared ? 0 : group % 4 == 0 ? 2 : group % 2 == 0 ? 1 : 0;
+    a.by_group = div_of(group >> a.together);
+    const uint32_t queries = few ? 32 : kQueries >> a.together;
     a.tiles = ((uint32_t)c.max_q + queries - 1) / queries;
-    const uint32_t wgs = a.tiles * pairs;                 // below 2^31: checked
+    const uint32_t wgs = a.tiles * (pairs >> a.together); // below 2^31: checked
     for (a.first_wg = 0; a.first_wg < wgs; a.first_wg += kLaunchMost) {
         const uint32_t grid = std::min(wgs - a.first_wg, kLaunchMost);
         hipError_t e;

@@ -97,6 +97,16 @@ def test_long_prompts(n, dim, variant, heads, causal):
     _packed(rng, [n], [n + (37 if causal else 0)], heads, heads // 2, dim, _attention(rng, dim, 27 * 27 * dim ** 0.5, variant, causal, keys=n))
 
 
+@pytest.mark.parametrize("heads,kv_heads", [(160, 40), (120, 10), (84, 42), (63, 21), (64, 1)])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+def test_heads_that_share_a_workgroup(heads, kv_heads, dim):
+    """Four heads, two or one to a workgroup; sequences of every remainder, of one tile and of several."""
+    rng = np.random.default_rng([heads, dim])
+    p = _attention(rng, dim, 27 * 27 * dim ** 0.5, 1, int(rng.integers(2)), keys=100)
+    _packed(rng, [200, 1, 31, 33, 95, 129, 64], [200, 1, 40, 33, 95, 160, 64], heads, kv_heads, dim, p, offset=3)
+    _packed(rng, [60, 1, 31, 33, 8, 64, 2, 50], [60, 1, 40, 20, 8, 64, 130, 50], heads, kv_heads, dim, p)
+
+
 @pytest.mark.parametrize("n,k", [(1, 1), (3, 508), (5, 509), (1, 3000), (32, 255), (33, 256), (2, 257), (4, 2049)])
 def test_few_queries_of_many_keys(n, k):
     """Keys divided over wavefronts: around one block each, and where a sum no longer fits with its upper half in one."""
