@@ -216,17 +216,18 @@ static void rmsnorm_rows(const RmsnormCall &c, int64_t first, int64_t rows, hipS
     // each took longer whatever the number of rows: 1 x 4096 4.7 in place of 3.9 us, 1000 x 4096 14.6 and 10.2, as did two
     // (1 x 2048 3.7 and 3.2).  Rows of 513 to 1024 values: four wavefronts and one chunk each where latency counts (200 x 768 3.4, one wavefront
     // 4.0 us), one from 512 rows on (1000 x 768 4.4 and 4.8, 8192 x 768 15.5 and 19.1).
-    if (chunks <= 64) rmsnorm_launch<1, 1>(a, fast, stream);
-    else if (chunks <= 128) rmsnorm_launch<1, 2>(a, fast, stream);
-    else if (chunks <= 256 && rows >= 512) rmsnorm_launch<1, 4>(a, fast, stream);
-    else if (chunks <= 256) rmsnorm_launch<4, 1>(a, fast, stream);
-    else if (chunks <= 512) rmsnorm_launch<4, 2>(a, fast, stream);
-    else if (chunks <= 768) rmsnorm_launch<4, 3>(a, fast, stream);
-    else if (chunks <= 1024) rmsnorm_launch<4, 4>(a, fast, stream);
-    else if (chunks <= 1280) rmsnorm_launch<4, 5>(a, fast, stream);
-    else if (chunks <= 1536) rmsnorm_launch<4, 6>(a, fast, stream);
-    else if (chunks <= 2048) rmsnorm_launch<4, 8>(a, fast, stream);
-    else if (chunks <= 3072) rmsnorm_launch<8, 6>(a, fast, stream);
+    auto fits = [&](int waves, int most) { return chunks <= 64 * waves * most; };
+    if (fits(1, 1)) rmsnorm_launch<1, 1>(a, fast, stream);
+    else if (fits(1, 2)) rmsnorm_launch<1, 2>(a, fast, stream);
+    else if (fits(1, 4) && rows >= 512) rmsnorm_launch<1, 4>(a, fast, stream);
+    else if (fits(4, 1)) rmsnorm_launch<4, 1>(a, fast, stream);
+    else if (fits(4, 2)) rmsnorm_launch<4, 2>(a, fast, stream);
+    else if (fits(4, 3)) rmsnorm_launch<4, 3>(a, fast, stream);
+    else if (fits(4, 4)) rmsnorm_launch<4, 4>(a, fast, stream);
+    else if (fits(4, 5)) rmsnorm_launch<4, 5>(a, fast, stream);
+    else if (fits(4, 6)) rmsnorm_launch<4, 6>(a, fast, stream);
+    else if (fits(4, 8)) rmsnorm_launch<4, 8>(a, fast, stream);
+    else if (fits(8, 6)) rmsnorm_launch<8, 6>(a, fast, stream);
     else rmsnorm_launch<8, 8>(a, fast, stream);
 }
 
