@@ -142,8 +142,9 @@ IPTQ_HD uint32_t floor_div_2_61(uint32_t den)
     return q;
 }
 
-// floor(c 2^n / den) for 32 <= n, c 2^n <= 2^54, den < 2^31 (0 for den == 0): the reciprocal is the first quotient, shifted; what it leaves
-// is below den + 6 c 2^(n - 31) < 2^32, so its low word, that of -q den, is all of it, and one more quotient is at most one short.
+// floor(c 2^n / den) for 32 <= n, c 2^n <= 2^54 (0 for den == 0): the reciprocal is the first quotient, shifted; what it leaves
+// is below den + 6 c 2^(n - 31), below 2^32 while den is below 2^31, so its low word, that of -q den, is all of it, and one more quotient is at
+// most one short.  (The weights of 131072 keys may add up to more than 2^31.)
 IPTQ_HD uint64_t floor_div_scaled(uint32_t c, int n, uint32_t den)
 {
     if (den == 0) return 0;
@@ -151,6 +152,7 @@ IPTQ_HD uint64_t floor_div_scaled(uint32_t c, int n, uint32_t den)
     const uint32_t r = reciprocal_of(den, k);
     uint64_t q = (uint64_t)r * c;
     q = down >= 0 ? q >> down : q << -down;
+    if (k == 0) return q + (((uint64_t)c << n) - q * den >= den ? 1 : 0);
     uint32_t left = 0u - (uint32_t)q * den;
     const uint32_t e = mulhi_u32(left, r) >> (31 - k);
     left -= e * den;

@@ -271,7 +271,8 @@ int main()
         if (floor_div_2_61(d) != (1ull << 61) / d) return printf("%u\n", d), 1;
     }
     for (long i = 0; i < 4000000; ++i) {
-        const uint32_t d = i < 600000 ? (uint32_t)i : i < 700000 ? 0x7fffffffu - (uint32_t)(i - 600000) : (uint32_t)(rnd() >> (33 + rnd() % 31));
+        const uint32_t d = i < 600000 ? (uint32_t)i : i < 700000 ? 0x80050000u - (uint32_t)(i - 600000) * 7 : i < 1200000 ? 0u - (uint32_t)(i - 700000) * 211
+                           : (uint32_t)(rnd() >> (32 + rnd() % 32));
         if (floor_div_scaled(1, 54, d) != (d ? (1ull << 54) / d : 0) || floor_div_scaled(127, 40, d) != (d ? (127ull << 40) / d : 0)) return printf("%u\n", d), 9;
     }
     for (long i = 0; i < 300000; ++i) {

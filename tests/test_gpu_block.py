@@ -330,6 +330,14 @@ def test_cache_attention_longest():
     _attend(rng, [n, 3], 2, 1, 32, page, 1, p)
 
 
+@pytest.mark.parametrize("i0", [1018, 1019])
+def test_cache_attention_every_weight_at_its_most(i0):
+    """Equal scores of as many keys as there may be: the weights add up to more than 2^31."""
+    rng = np.random.default_rng(i0)
+    p = ob.Attention(1, i0, 5, 0, 1, Dyadic(32000, 19, 0, -128, 127))
+    _attend(rng, [131072, 70000, 131071], 3, 1, 32, 256, 1, p, sigma=0)
+
+
 @pytest.mark.parametrize("dim", [32, 64, 96, 128])
 @pytest.mark.parametrize("page,heads", [(16, 5), (32, 3), (128, 4), (256, 20), (4096, 9)])
 def test_cache_attention_page_sizes(dim, page, heads):
